@@ -195,6 +195,108 @@ dmr_status_t dmr_qlinear_bf16_forward_fused(const uint16_t *d_w, dmr_prologue_t 
                                             void *stream);
 
 /*
+ * The attention block between the qkv projection and the output projection of a decoder layer, for serving: keys and values of
+ * all requests live in pages, and a step brings each request one new token (decode), a few (drafted tokens to verify) or many
+ * (a chunk of a prompt).  The paper's models (Sec. 5.1) are pre-norm decoders with grouped query heads, per-head norms of queries
+ * and keys and rotary positions; the paper does not restate these operations, they are taken in their textbook form.  Both copies
+ * of a model share one cache, so that a step may be routed either way (Eq. 1).
+ *
+ * A cache is two pools, d_k and d_v, of `pages` pages of dmr_kv_page_bytes each.  A page holds page_tokens tokens of every
+ * key / value head: [kv_heads][page_tokens / 16] blocks of 16 tokens x head_dim.  Inside a block the elements lie in pieces of 16
+ * bytes, pc elements each (8 of bf16, 16 of e4m3), in the order in which the matrix cores take them:
+ *   keys    [head_dim / pc][16 tokens][pc]         piece p of a token: its elements pc p .. pc p + pc - 1
+ *   values  [16 / pc][head_dim][pc tokens]         a piece: one element of pc consecutive tokens
+ * so pages can be copied, moved or shared whole without knowing more.  Token j of a request is token j % page_tokens of the page
+ * that entry j / page_tokens of the request's row of the block table names; a slot is page * page_tokens + the token's place in it.
+ *
+ * The int32 arrays of these calls need 4-byte alignment only, so that a call can take part of a batch from any request on.
+ * page_tokens: 16, 32, 64, 128 or 256.  head_dim: 64 or 128.  pages * page_tokens below 2^31.  DMR_KV_BF16 keeps the elements as
+ * they are (both scales 1); DMR_KV_E4M3 keeps x / scale in 8 bits (e4m3, to nearest even, past 448 the largest), one positive
+ * scale for the keys and one for the values of the layer.
+ */
+typedef enum {
+    DMR_KV_BF16 = 0,
+    DMR_KV_E4M3 = 1
+} dmr_kv_type_t;
+
+typedef struct {
+    void *d_k, *d_v;      /* pages x dmr_kv_page_bytes each, 16-byte aligned */
+    int64_t pages;
+    int32_t page_tokens, kv_heads, head_dim;
+    dmr_kv_type_t type;
+    float k_scale, v_scale;
+} dmr_kv_cache_t;
+
+/* Bytes of one page in one of the two pools; 0 if the layout is not supported. */
+size_t dmr_kv_page_bytes(int32_t page_tokens, int32_t kv_heads, int32_t head_dim, dmr_kv_type_t type);
+
+/*
+ * Block tables and slots of a step from the requests' lengths, on the GPU, so that a captured graph can take pages by itself.
+ * Request b (0 .. requests - 1) has d_lens[b] tokens in the cache, in ceil(d_lens[b] / page_tokens) pages, and brings
+ * d_new_tokens[b] more (a negative count is read as 0); its rows of the step follow those of request b - 1.  The pages it
+ * needs are taken from the top of a stack: the n-th page taken by the call is d_free_pages[free - 1 - n], free = *d_free_count
+ * (read as 0 .. free_capacity), and is entered in its row of the table behind its last page.
+ *   d_block_table [requests][table_width]  in and out; entries other than those of new pages are left as they were
+ *   d_query_start [requests + 1]           first row of each request, and the end of the last
+ *   d_kv_lens     [requests]               tokens in the cache after the step
+ *   d_positions, d_slots [rows]            of each row
+ *   d_left        [2]                      pages left on the stack, requests refused
+ * A request is refused when its tokens pass the table's width or its rows pass `rows`, or when it needs a page and its own and
+ * all earlier needs (those refused for want of pages included, the others not) pass the stack.  It takes no page, its length comes
+ * out as -1 - length, which this call reads as `length` again and dmr_attn_paged as no keys, and its rows get position 0 and
+ * slot -1, as do rows behind the last request.  d_kv_lens may be d_lens, and d_left may begin at d_free_count (2 words): then a
+ * step updates the program's own state.  The other arrays are apart.  d_query_start never passes `rows`.
+ * At most 2^20 requests and 2^22 rows; table_width * page_tokens below 2^31.
+ */
+dmr_status_t dmr_kv_assign(int64_t requests, int64_t rows, int64_t table_width, int32_t page_tokens, int64_t free_capacity,
+                           const int32_t *d_new_tokens, const int32_t *d_lens, const int32_t *d_free_pages,
+                           const int32_t *d_free_count, int32_t *d_block_table, int32_t *d_query_start,
+                           int32_t *d_kv_lens, int32_t *d_positions, int32_t *d_slots, int32_t *d_left, void *stream);
+
+/*
+ * The output of the fused qkv projection to queries, and to keys and values in the cache.  d_qkv is bf16
+ * [rows][(q_heads + 2 kv_heads) head_dim]: the query heads, the key heads, the value heads.  In fp32, rounded once at the end:
+ *   norm       y = x * gamma / sqrt(mean(x^2) + eps) over each query (key) head, if d_gamma_q (d_gamma_k), bf16 [head_dim], is
+ *              not NULL; a head of zeros stays zeros
+ *   rotation   if d_inv_freq, fp32 [head_dim / 2], is not NULL: pair i of each query and key head turns by the angle
+ *              position * inv_freq[i] (the product is exact enough at any position): (a, b) to (a cos - b sin, b cos + a sin).
+ *              A pair is the elements i, i + head_dim / 2 (DMR_ROPE_HALVES) or 2 i, 2 i + 1 (DMR_ROPE_ADJACENT).
+ * Queries go to d_q, bf16 [rows][q_heads head_dim]; keys and values of row t to slot d_slots[t] of the cache; a row whose slot is
+ * negative or not in the cache is not written there.  Slots of one call are distinct.  d_positions may be NULL without a rotation.
+ */
+typedef enum {
+    DMR_ROPE_HALVES = 0,
+    DMR_ROPE_ADJACENT = 1
+} dmr_rope_t;
+
+dmr_status_t dmr_kv_append(const dmr_kv_cache_t *cache, const uint16_t *d_qkv, int64_t rows, int32_t q_heads,
+                           const uint16_t *d_gamma_q, const uint16_t *d_gamma_k, float eps, const float *d_inv_freq,
+                           dmr_rope_t pairs, const int32_t *d_positions, const int32_t *d_slots, uint16_t *d_q, void *stream);
+
+/*
+ * Attention of the step's rows over the cache, causal.  Request b has the n = d_query_start[b + 1] - d_query_start[b] rows from
+ * d_query_start[b] on, the last n of its d_kv_lens[b] keys (dmr_kv_append has written them): its row i sees the keys
+ * 0 .. d_kv_lens[b] - n + i, and query head h the keys of head h / (q_heads / kv_heads):
+ *   out[i][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * (q[i][h] . k_j))
+ * d_q and d_out are bf16 [rows][q_heads head_dim] and apart, d_block_table is [requests][table_width].  A row that sees no key is 0; rows before
+ * the first request and behind the last are left as they were.  max_query is at least the largest n (rows of a request past it
+ * are not computed); it chooses the kernel, so a decode step passes 1.  Scores, sums and outputs are held in fp32; of the weights
+ * p_j the product with the values takes 8 bits, as the values have, and the sum that divides it the same ones.
+ * Lengths past the table are read as its width, entries of the table outside the cache as its first or last page; slots
+ * behind a request's last key may hold anything, NaN included.  Non-finite keys and values that a request does hold are outside
+ * the contract.
+ * d_ws as dmr_attn_paged_workspace_bytes says: partial results where the keys of a request are split over workgroups.  It may
+ * arrive uninitialised.  The lengths are read on the device alone: a captured call serves any lengths that `rows`, the table
+ * and max_query admit.
+ */
+size_t dmr_attn_paged_workspace_bytes(int64_t rows, int64_t requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                      int64_t max_query);
+dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, int64_t rows, int32_t q_heads, int64_t requests,
+                            const int32_t *d_query_start, const int32_t *d_kv_lens, const int32_t *d_block_table,
+                            int64_t table_width, int64_t max_query, float scale, uint16_t *d_out, void *d_ws, size_t ws_bytes,
+                            void *stream);
+
+/*
  * Offline step that produces the low-precision copy (App. E names AWQ/GPTQ; this is plain
  * asymmetric round-to-nearest, which yields the same format): fp32 weights [N][K] to canonical
  * qweight / scales / zeros.  Per (row, group): lo = min(w, 0), hi = max(w, 0),

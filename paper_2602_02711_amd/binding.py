@@ -30,10 +30,20 @@ EXPORTS = (
     "dmr_qlinear_bf16_fused_workspace_bytes", "dmr_qlinear_forward_fused", "dmr_qlinear_bf16_forward_fused",
     "dmr_qlinear_kernel_path", "dmr_qlinear_forward_static", "dmr_probe_empty_launch",
     "dmr_qlinear_per_channel_storage_bytes",
+    "dmr_kv_page_bytes", "dmr_kv_assign", "dmr_kv_append", "dmr_attn_paged_workspace_bytes", "dmr_attn_paged",
 )
 
 DMR_PRO_NONE, DMR_PRO_RMSNORM, DMR_PRO_SWIGLU = 0, 1, 2
 DMR_FMT_W4_G128, DMR_FMT_W4_PER_CHANNEL, DMR_FMT_W3_G128, DMR_FMT_BF16 = 0, 1, 2, 3
+DMR_KV_BF16, DMR_KV_E4M3 = 0, 1
+DMR_ROPE_HALVES, DMR_ROPE_ADJACENT = 0, 1
+
+
+class _KvCacheStruct(ctypes.Structure):
+    """dmr_kv_cache_t"""
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("type", ctypes.c_int), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float)]
 
 
 class DmrError(RuntimeError):
@@ -109,6 +119,17 @@ def lib() -> ctypes.CDLL:
         L.dmr_qlinear_bf16_forward_fused.restype = ctypes.c_int
         L.dmr_qlinear_bf16_forward_fused.argtypes = [vp, ctypes.c_int, vp, vp, f32, vp, i64, i64, i64, vp,
                                                      ctypes.c_int, vp, sz, vp]
+        cache = ctypes.POINTER(_KvCacheStruct)
+        L.dmr_kv_page_bytes.restype = sz
+        L.dmr_kv_page_bytes.argtypes = [i32, i32, i32, ctypes.c_int]
+        L.dmr_kv_assign.restype = ctypes.c_int
+        L.dmr_kv_assign.argtypes = [i64, i64, i64, i32, i64] + [vp] * 11
+        L.dmr_kv_append.restype = ctypes.c_int
+        L.dmr_kv_append.argtypes = [cache, vp, i64, i32, vp, vp, f32, vp, ctypes.c_int, vp, vp, vp, vp]
+        L.dmr_attn_paged_workspace_bytes.restype = sz
+        L.dmr_attn_paged_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i64]
+        L.dmr_attn_paged.restype = ctypes.c_int
+        L.dmr_attn_paged.argtypes = [cache, vp, i64, i32, i64, vp, vp, vp, i64, i64, f32, vp, vp, sz, vp]
         L.dmr_status_string.restype = ctypes.c_char_p
         L.dmr_status_string.argtypes = [ctypes.c_int]
         L.dmr_qlinear_kernel_path.restype = ctypes.c_char_p
@@ -456,4 +477,148 @@ def dmr_qlinear_bf16_forward_fused(w: torch.Tensor, pro: int, inp: torch.Tensor,
     pws, wbytes = _workspace(workspace)
     _check(lib().dmr_qlinear_bf16_forward_fused(pw_, pro, pi, pg, float(eps), pr, M, K, N, po, _out_code(out.dtype),
                                                 pws, wbytes, _stream(stream)), "dmr_qlinear_bf16_forward_fused")
+    return out
+
+
+# ---- paged attention -----------------------------------------------------------------------------
+
+_I32 = (torch.int32,)
+
+
+def _here(*tensors) -> None:
+    """The tensors of a call share the current device."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and (t.device if isinstance(t, KvCache) else t.get_device()) != dev:
+            raise ValueError("all tensors must be on the current device")
+
+
+class KvCache:
+    """One layer's keys and values in pages: the pools of ``dmr_kv_cache_t``, bf16 or float8_e4m3fn (16-byte pieces of ``pc``
+    elements), k ``[pages][kv_heads][page_tokens / 16][head_dim / pc][16][pc]``, v ``[pages][kv_heads][page_tokens / 16][16 / pc][head_dim][pc]``."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: float = 1.0, v_scale: float = 1.0):
+        types = (torch.bfloat16, torch.float8_e4m3fn)
+        pk, pv = _dev(k, "k", types), _dev(v, "v", types)
+        if k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must have one dtype and one device")
+        pc = 16 // k.element_size()
+        if k.dim() != 6 or tuple(k.shape[4:]) != (16, pc):
+            raise ValueError("k must be [pages][kv_heads][page_tokens / 16][head_dim / %d][16][%d]" % (pc, pc))
+        pages, heads, blocks, pieces = k.shape[:4]
+        if tuple(v.shape) != (pages, heads, blocks, 16 // pc, pieces * pc, pc):
+            raise ValueError("v must be [pages][kv_heads][page_tokens / 16][%d][head_dim][%d]" % (16 // pc, pc))
+        self.k, self.v, self.device = k, v, k.get_device()
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim = pages, 16 * blocks, heads, pieces * pc
+        self.k_scale, self.v_scale = float(k_scale), float(v_scale)
+        kind = DMR_KV_BF16 if k.dtype == torch.bfloat16 else DMR_KV_E4M3
+        self._struct = _KvCacheStruct(pk, pv, pages, self.page_tokens, heads, self.head_dim, kind, self.k_scale, self.v_scale)
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, pages: int, page_tokens: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, k_scale: float = 1.0,
+              v_scale: float = 1.0, device="cuda") -> "KvCache":
+        """A cache on uninitialised pools of its own."""
+        if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise TypeError("a cache is torch.bfloat16 or torch.float8_e4m3fn")
+        pc = 8 if dtype == torch.bfloat16 else 16
+        if dmr_kv_page_bytes(page_tokens, kv_heads, head_dim, DMR_KV_BF16 if pc == 8 else DMR_KV_E4M3) == 0:
+            raise ValueError("page_tokens, kv_heads or head_dim not supported")
+        head = (pages, kv_heads, page_tokens // 16)
+        return cls(torch.empty(head + (head_dim // pc, 16, pc), dtype=dtype, device=device),
+                   torch.empty(head + (16 // pc, head_dim, pc), dtype=dtype, device=device), k_scale, v_scale)
+
+
+def dmr_kv_page_bytes(page_tokens: int, kv_heads: int, head_dim: int, kind: int) -> int:
+    return int(lib().dmr_kv_page_bytes(page_tokens, kv_heads, head_dim, kind))
+
+
+def dmr_kv_assign(new_tokens: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                  block_table: torch.Tensor, page_tokens: int, rows: int, out=None, stream=None):
+    """(query_start, kv_lens, positions, slots, left), all int32; ``block_table`` gets the new pages.  ``out``: the five tensors to
+    write; its kv_lens may be ``lens``, and its left may share its first word with ``free_count``."""
+    pn, pl = _dev(new_tokens, "new_tokens", _I32), _dev(lens, "lens", _I32)
+    pf, pc, pt = _dev(free_pages, "free_pages", _I32), _dev(free_count, "free_count", _I32), _dev(block_table, "block_table", _I32)
+    n = new_tokens.numel()
+    if lens.numel() != n or free_count.numel() < 1 or block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("lens must hold a value per request, block_table be [requests][width], free_count hold one value")
+    if rows < 0:
+        raise ValueError("rows must not be negative")
+    if out is None:
+        out = tuple(torch.empty(m, dtype=torch.int32, device=lens.device) for m in (n + 1, n, rows, rows, 2))
+    ps, pk, pp, po, pe = (_dev(t, "out", _I32) for t in out)
+    if [t.numel() for t in out] != [n + 1, n, rows, rows, 2]:
+        raise ValueError("out must be query_start [requests + 1], kv_lens [requests], positions [rows], slots [rows], left [2]")
+    _here(new_tokens, lens, free_pages, free_count, block_table, *out)
+    _check(lib().dmr_kv_assign(n, rows, block_table.shape[1], page_tokens, free_pages.numel(), pn, pl, pf, pc, pt, ps, pk, pp, po, pe,
+                               _stream(stream)), "dmr_kv_assign")
+    return tuple(out)
+
+
+def dmr_kv_append(cache: KvCache, qkv: torch.Tensor, q_heads: int, positions: torch.Tensor | None, slots: torch.Tensor,
+                  gamma_q: torch.Tensor | None = None, gamma_k: torch.Tensor | None = None, eps: float = 0.0,
+                  inv_freq: torch.Tensor | None = None, interleaved: bool = False, out: torch.Tensor | None = None,
+                  stream=None) -> torch.Tensor:
+    """qkv [rows][(q_heads + 2 kv_heads) head_dim] to queries [rows][q_heads head_dim] (returned) and to the cache's slots."""
+    px, ps = _dev(qkv, "qkv", _BF16), _dev(slots, "slots", _I32)
+    D = cache.head_dim
+    if qkv.dim() != 2 or qkv.shape[1] != (q_heads + 2 * cache.kv_heads) * D:
+        raise ValueError("qkv must be [rows][(q_heads + 2 kv_heads) head_dim]")
+    rows = qkv.shape[0]
+    if slots.numel() != rows:
+        raise ValueError("slots must hold one value per row")
+    pp = pg = ph = pf = None
+    if positions is not None:
+        pp = _dev(positions, "positions", _I32)
+        if positions.numel() != rows:
+            raise ValueError("positions must hold one value per row")
+    if gamma_q is not None:
+        pg = _dev(gamma_q, "gamma_q", _BF16)
+    if gamma_k is not None:
+        ph = _dev(gamma_k, "gamma_k", _BF16)
+    if any(g is not None and tuple(g.shape) != (D,) for g in (gamma_q, gamma_k)):
+        raise ValueError("gamma_q and gamma_k must be [head_dim]")
+    if inv_freq is not None:
+        pf = _dev(inv_freq, "inv_freq", (torch.float32,))
+        if tuple(inv_freq.shape) != (D // 2,):
+            raise ValueError("inv_freq must be [head_dim / 2]")
+    if out is None:
+        out = torch.empty((rows, q_heads * D), dtype=torch.bfloat16, device=qkv.device)
+    po = _dev(out, "out", _BF16)
+    if tuple(out.shape) != (rows, q_heads * D):
+        raise ValueError("out must be [rows][q_heads head_dim]")
+    _here(cache, qkv, slots, positions, gamma_q, gamma_k, inv_freq, out)
+    _check(lib().dmr_kv_append(cache._ref, px, rows, q_heads, pg, ph, float(eps), pf, DMR_ROPE_ADJACENT if interleaved else DMR_ROPE_HALVES,
+                               pp, ps, po, _stream(stream)), "dmr_kv_append")
+    return out
+
+
+def dmr_attn_paged_workspace_bytes(rows: int, requests: int, q_heads: int, kv_heads: int, head_dim: int, max_query: int) -> int:
+    return int(lib().dmr_attn_paged_workspace_bytes(rows, requests, q_heads, kv_heads, head_dim, max_query))
+
+
+def dmr_attn_paged(cache: KvCache, q: torch.Tensor, q_heads: int, query_start: torch.Tensor, kv_lens: torch.Tensor,
+                   block_table: torch.Tensor, max_query: int, scale: float, out: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of rows q [rows][q_heads head_dim] over their requests' keys in the cache.  A new ``out`` is zeroed, since
+    rows of no request are not written."""
+    pq, ps, pl, pt = _dev(q, "q", _BF16), _dev(query_start, "query_start", _I32), _dev(kv_lens, "kv_lens", _I32), _dev(block_table, "block_table", _I32)
+    n, D = kv_lens.numel(), cache.head_dim
+    if q.dim() != 2 or q.shape[1] != q_heads * D:
+        raise ValueError("q must be [rows][q_heads head_dim]")
+    if query_start.numel() != n + 1 or block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError("query_start must be [requests + 1], block_table [requests][width]")
+    if out is None:
+        out = torch.zeros((q.shape[0], q_heads * D), dtype=torch.bfloat16, device=q.device)
+    po = _dev(out, "out", _BF16)
+    if tuple(out.shape) != tuple(q.shape):
+        raise ValueError("out must be [rows][q_heads head_dim]")
+    _here(cache, q, query_start, kv_lens, block_table, out, workspace)
+    if workspace is None:
+        need = dmr_attn_paged_workspace_bytes(q.shape[0], n, q_heads, cache.kv_heads, D, max_query)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)    # device memory only
+    pw, wbytes = _workspace(workspace)
+    _check(lib().dmr_attn_paged(cache._ref, pq, q.shape[0], q_heads, n, ps, pl, pt, block_table.shape[1], max_query, float(scale), po, pw,
+                                wbytes, _stream(stream)), "dmr_attn_paged")
     return out

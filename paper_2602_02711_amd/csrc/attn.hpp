@@ -1,0 +1,92 @@
+// The attention block's shared declarations: how the paged cache lies in memory, what the kernels are given, and the launchers.
+//
+// Layout of a pool: [page][kv head][16-token block], a block 16 x D elements in pieces of 16 bytes (pc elements: 8 bf16, 16 e4m3),
+// keys [D / pc][16][pc], values [16 / pc][D][pc].  It is the order of MFMA operands: with scores formed as K Q^T and outputs as
+// V^T P^T both products take the cache as their A operand, 8 elements along the contraction per lane, so a wave fetches an operand
+// as whole pieces that lie side by side, straight into registers, and no transposition is left for the kernels.  The scores come
+// out of the first product with a query per lane column and keys along the registers, which is how the second one wants its B
+// operand once the keys are taken in the matching order (key_of_row in the kernels): probabilities never leave their lane.
+#pragma once
+#include "common.hpp"
+
+namespace dmr {
+
+constexpr int kBlockTokens = 16;      // tokens of a cache block
+constexpr int kUnit = 64;             // keys that a kernel takes at a time
+
+struct AttnArgs {
+    const uint16_t *q;
+    uint16_t *out;
+    const uint8_t *k, *v;
+    const int32_t *start, *lens, *table;
+    float *part;              // [item][kv head][tile rows][D] unnormalised outputs
+    float2 *ml;               // [item][kv head][tile rows]: largest score (log2 units), sum
+    int32_t rows, requests, width, q_heads, kv_heads, G, pages, page_shift;
+    float scale_log2;         // softmax scale * key scale * log2(e)
+    float v_scale;
+    int32_t items;            // per kv head, of the grid
+    int32_t parts;            // attn_tiles: parts of a tile's keys;  attn_few: see share_of_item, 0 for one item per request
+};
+
+// A request as its device arrays have it, kept inside the buffers whatever they hold.
+struct Request {
+    int first, n, keys;       // rows first .. first + n - 1, the last n of `keys` keys
+};
+__device__ __forceinline__ Request request_at(const AttnArgs &a, int b) {
+    Request r;
+    r.first = min(max(a.start[b], 0), a.rows);
+    r.n = min(max(a.start[b + 1], r.first), a.rows) - r.first;
+    r.keys = min(max(a.lens[b], 0), a.width << a.page_shift);
+    return r;
+}
+
+// First byte of a block of 16 tokens of one head: `block` of the request whose row of the table is given.
+template <int BLOCK_BYTES>
+__device__ __forceinline__ int64_t block_offset(const AttnArgs &a, const int32_t *row, int block, int head) {
+    const int per_page = a.page_shift - 4;
+    const int page = min(max(row[block >> per_page], 0), a.pages - 1);
+    return (((((int64_t)page * a.kv_heads + head) << per_page) + (block & ((1 << per_page) - 1)))) * BLOCK_BYTES;
+}
+
+// Eight e4m3 bytes to eight bf16 (exact).
+__device__ __forceinline__ uint4 bf16_of_e4m3(uint32_t lo, uint32_t hi) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
+    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
+    // a bf16 is the high half of its fp32: no rounding to do
+    auto pair = [](f32x2 p) { return __builtin_amdgcn_perm(__float_as_uint(p[1]), __float_as_uint(p[0]), 0x07060302u); };
+    return make_uint4(pair(a), pair(b), pair(c), pair(d));
+}
+
+// 2^x, x <= 0 or -inf.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kNoKey = -3.0e38f;    // "largest score" of a row that has seen no key: finite, so that differences stay numbers
+
+struct CacheView {
+    uint8_t *k, *v;
+    int64_t pages;
+    int32_t page_shift, kv_heads, D;
+    bool e4m3;
+    float k_scale, v_scale;
+};
+
+hipError_t launch_kv_assign(int64_t requests, int64_t rows, int64_t width, int page_shift, int64_t capacity, const int32_t *new_tokens,
+                            const int32_t *lens, const int32_t *free_pages, const int32_t *free_count, int32_t *table,
+                            int32_t *start, int32_t *kv_lens, int32_t *positions, int32_t *slots, int32_t *left, hipStream_t stream);
+hipError_t launch_kv_append(const CacheView &c, const uint16_t *qkv, int64_t rows, int q_heads, const uint16_t *gamma_q,
+                            const uint16_t *gamma_k, float eps, const float *inv_freq, bool adjacent, const int32_t *positions,
+                            const int32_t *slots, uint16_t *q, hipStream_t stream);
+
+// How a call of dmr_attn_paged is split, from what the host knows: pure arithmetic, the same for the workspace query and the launch.
+struct AttnPlan {
+    int tile_rows;            // (token, query head) rows of a tile
+    int64_t items;            // workgroups per kv head
+    int parts;                // AttnArgs::parts
+    bool split;               // several items may belong to one tile: partial results, joined by a second kernel
+};
+AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query);
+inline size_t attn_part_floats(const AttnPlan &p, int kv_heads, int D) { return (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows * (size_t)D; }
+hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream);
+hipError_t launch_attn_join(const AttnArgs &a, int tile_rows, int D, hipStream_t stream);
+
+}  // namespace dmr

@@ -1,0 +1,225 @@
+"""dmr_attn_paged against the definition in 64 bits.
+
+Tolerance of an element, with A = sum p |v| / sum p.  A score is off by at most (dim + 4) 2^-24 of scale sum |q k| (products of bf16 are
+exact in fp32, their sum is not; then the scale, and in the exponent's log2 units), so a weight by e = (dim + 16) 2^-23 (1 + that
+sum) of itself, exponential included.  The kernel rounds each weight to 8 bits, r = 2^-8, and divides by the sum of these:
+numerator and denominator move by (r + e) of A and of the result.  The sums' own roundings, at most keys 2^-24 of A, stand in a
+factor of 2 on e.  Then one rounding to bf16, 2^-8 of the result."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_02711_amd as dmr
+
+import attn_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+K_SCALE, V_SCALE = 0.05, 0.013
+SENTINEL = 123.0
+
+
+def dev(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+def build(seed, news, lens, heads, kv_heads, dim, page, cache, sharp=2.0, extra_cols=1, spare=2):
+    """A cache with the requests' keys in shuffled pages, NaN in every slot that holds none, -1 behind the tables' last entries."""
+    gen = torch.Generator().manual_seed(seed)
+    held = [-(-max(l, 0) // page) for l in lens]
+    pages = sum(held) + spare
+    width = max(held + [1]) + extra_cols
+    order = torch.randperm(pages, generator=gen).numpy()
+    ks, vs = (1.0, 1.0) if cache == "bf16" else (K_SCALE, V_SCALE)
+    k = torch.full((pages * page, kv_heads, dim), float("nan"))
+    v = torch.full((pages * page, kv_heads, dim), float("nan"))
+    table = np.full((len(lens), width), -1, np.int64)
+    dt = ref.dtype_of(cache)
+    keys, at = [], 0
+    for b, l in enumerate(lens):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+        l = max(l, 0)
+        kb = (torch.randn(l, kv_heads, dim, generator=gen) / ks).to(dt)
+        vb = ((torch.randn(l, kv_heads, dim, generator=gen) + 0.3) / vs).to(dt)
+        t = torch.arange(l)
+        slot = torch.from_numpy(table[b])[t // page] * page + t % page
+        k[slot], v[slot] = kb.float(), vb.float()
+        keys.append((kb.double() * ks, vb.double() * vs))
+    kp, vp = ref.pack(k.view(pages, page, kv_heads, dim), v.view(pages, page, kv_heads, dim), cache)
+    q = (torch.randn(sum(news), heads * dim, generator=gen) * sharp).bfloat16()
+    pool = dmr.KvCache(kp.to(dt).to(DEV), vp.to(dt).to(DEV), ks, vs)
+    return pool, q, keys, table
+
+
+def expect(q, keys, news, heads, dim, scale, r):
+    out, tol, at = [], [], 0
+    for (kb, vb), n in zip(keys, news):
+        o, size, score = ref.attend(q[at:at + n].view(n, heads, dim), kb, vb, n, scale)
+        e = 2 * (dim + 16) * 2.0 ** -23 * (1 + score)
+        out.append(o)
+        tol.append((r + e) * (size + o.abs()) * 1.01 + ref.BF16_STEP * o.abs())
+        at += n
+    return torch.cat(out), torch.cat(tol)
+
+
+def check(seed, news, lens, heads, kv_heads, dim, page, cache, sharp=2.0, pad=3, most=None, **more):
+    pool, q, keys, table = build(seed, news, lens, heads, kv_heads, dim, page, cache, sharp, **more)
+    rows, scale = sum(news), dim ** -0.5
+    most = max(max(news), 1) if most is None else most
+    start = np.concatenate([[0], np.cumsum(news)])
+    qp = torch.cat([q, torch.full((pad, heads * dim), float("nan"), dtype=torch.bfloat16)]).to(DEV)
+    out = torch.full_like(qp, SENTINEL)
+    need = dmr.dmr_attn_paged_workspace_bytes(rows + pad, len(news), heads, kv_heads, dim, most)
+    ws = torch.full((need + 16,), 0xFF, dtype=torch.uint8, device=DEV)          # NaN wherever it is read before it is written
+    dmr.dmr_attn_paged(pool, qp, heads, dev(start), dev(lens), dev(table), most, scale, out=out, workspace=ws[:max(need, 16)])
+    assert (ws[max(need, 16):] == 0xFF).all()
+    assert (out[rows:] == SENTINEL).all()
+    # a request of no keys sees none of its rows; one of fewer keys than rows, only the last
+    want, tol = expect(q, keys, news, heads, dim, scale, 2.0 ** -8)
+    got = out[:rows].cpu().double().view(rows, heads, dim)
+    assert torch.isfinite(got).all()
+    over = (got - want).abs() - tol
+    assert rows == 0 or over.max() <= 0, f"{over.max():.3g} past the tolerance; largest error {(got - want).abs().max():.3g}"
+    return pool, qp, out, dev(start), dev(lens), dev(table), most, scale
+
+
+ONE = [(1, 16), (15, 16), (16, 16), (17, 16), (63, 32), (64, 64), (65, 64), (255, 16), (257, 256), (1003, 64), (4097, 128)]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("keys,page", ONE)
+def test_one_token(keys, page, cache):
+    check(keys, [1], [keys], 8, 2, 128, page, cache)
+    check(keys + 1, [1], [keys], 3, 1, 64, page, cache)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (4, 4, 128), (5, 1, 128), (14, 2, 64), (8, 1, 128), (16, 1, 64), (32, 2, 128),
+                                                (17, 1, 64), (32, 1, 128), (33, 1, 64), (71, 1, 64)])
+def test_head_layouts_of_a_decode_batch(heads, kv_heads, dim, cache):
+    check(heads, [1] * 7, [1, 700, 64, 129, 3000, 17, 300], heads, kv_heads, dim, 32, cache)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("news,lens", [
+    ([3, 1, 5], [3, 70, 900]),
+    ([8, 8, 2, 8], [200, 8, 1500, 64]),
+    ([0, 4, 0, 1, 0], [50, 60, 0, 1, 7]),
+    ([33], [33]), ([64], [64]), ([65], [1000]), ([200, 1, 90], [200, 400, 91]), ([0, 130], [3, 515])])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(8, 2, 128, 64), (6, 2, 64, 16), (4, 4, 64, 32), (5, 1, 128, 128)])
+def test_several_tokens(news, lens, heads, kv_heads, dim, page, cache):
+    check(len(news) + heads, news, lens, heads, kv_heads, dim, page, cache)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("news,lens", [([1, 1, 1], [0, -1, -200]), ([4, 4, 4], [0, 2, -5]), ([90, 70, 60], [0, 50, 1])])
+def test_rows_that_see_no_key_are_zero(news, lens, cache):
+    _, _, out, start, *_ = check(3, news, lens, 8, 2, 128, 16, cache)
+    first = start.tolist()
+    for b, (n, l) in enumerate(zip(news, lens)):
+        blind = n - max(l, 0)
+        assert blind <= 0 or (out[first[b]:first[b] + blind] == 0).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_long_chunk(dim, cache):
+    check(dim, [700], [2500], 8, 2, dim, 64, cache)
+    check(dim + 1, [260, 515], [260, 3001], 2, 1, dim, 16, cache)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("requests", [64, 65, 150])
+def test_many_requests(requests, cache):
+    rng = np.random.default_rng(requests)
+    check(requests, [1] * requests, rng.integers(0, 400, requests).tolist(), 4, 1, 64, 16, cache)
+    news = rng.integers(0, 40, requests).tolist()
+    check(requests, news, [n + int(o) for n, o in zip(news, rng.integers(0, 90, requests))], 4, 2, 64, 16, cache)
+
+
+@pytest.mark.parametrize("sharp", [0.0, 0.01, 30.0])
+@pytest.mark.parametrize("news,lens", [([1, 1], [900, 5000]), ([4], [700]), ([150], [600])])
+def test_flat_and_sharp_scores(news, lens, sharp):
+    check(7, news, lens, 8, 2, 128, 64, "bf16", sharp)
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1, 1], [1, 300, 2000]), ([6, 3], [6, 700]), ([100, 30], [500, 30])])
+def test_max_query_larger_than_any_request(news, lens):
+    for most in (max(news), 9, 40, 1000):
+        check(11, news, lens, 4, 1, 128, 32, "bf16", most=max(most, max(news)))
+
+
+@pytest.mark.parametrize("news,lens", [([1] * 5, [800, 3000, 1, 64, 511]), ([5, 5], [900, 70]), ([150, 90], [4000, 90])])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_repeated_and_captured(news, lens, cache):
+    """The same bits again eagerly, on another stream, and from a graph replayed with other lengths in between."""
+    pool, q, out, start, kv, table, most, scale = check(13, news, lens, 8, 2, 128, 64, cache)
+    want = out.clone()
+    need = dmr.dmr_attn_paged_workspace_bytes(q.shape[0], len(news), 8, 2, 128, most)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device=DEV)
+    call = lambda: dmr.dmr_attn_paged(pool, q, 8, start, kv, table, most, scale, out=out, workspace=ws)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out.fill_(SENTINEL)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    full = kv.clone()
+    shorter = torch.maximum(kv // 2, (start[1:] - start[:-1]).to(kv.dtype))
+    for _ in range(3):
+        out.fill_(SENTINEL)
+        kv.copy_(shorter)
+        graph.replay()
+        torch.cuda.synchronize()
+        half = out.clone()
+        out.fill_(SENTINEL)
+        call()
+        assert torch.equal(out, half)
+        kv.copy_(full)
+        out.fill_(SENTINEL)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_pages_shared_by_requests():
+    """Two requests whose first pages are the same ones."""
+    pool, q, keys, table = build(21, [1, 1], [200, 130], 4, 2, 64, 64, "bf16")
+    table[1, :2] = table[0, :2]
+    keys[1] = tuple(torch.cat([a[:128], b[128:]]) for a, b in zip(keys[0], keys[1]))
+    out = dmr.dmr_attn_paged(pool, q.to(DEV), 4, dev([0, 1, 2]), dev([200, 130]), dev(table), 1, 0.125)
+    want, tol = expect(q, keys, [1, 1], 4, 64, 0.125, 2.0 ** -8)
+    assert ((out.cpu().double().view(2, 4, 64) - want).abs() <= tol).all()
+
+
+def test_entries_and_lengths_out_of_range_stay_in_the_cache():
+    """Whatever the device arrays hold, reads stay inside: the other requests' rows are right."""
+    pool, q, keys, table = build(22, [1, 1, 1], [200, 130, 90], 4, 2, 64, 64, "bf16", spare=0)
+    for t in (pool.k, pool.v):
+        t.nan_to_num_(0.0)
+    table[1] = [10 ** 6, -5, 2 ** 31 - 1, -2 ** 31, 77][:table.shape[1]]
+    out = dmr.dmr_attn_paged(pool, q.to(DEV), 4, dev([0, 1, 2, 3]), dev([200, 2 ** 31 - 1, 90]), dev(table), 1, 0.125)
+    want, tol = expect(q, keys, [1, 1, 1], 4, 64, 0.125, 2.0 ** -8)
+    ok = (out.cpu().double().view(3, 4, 64) - want).abs() <= tol
+    assert ok[0].all() and ok[2].all() and torch.isfinite(out).all()
+
+
+def test_cache_past_32_bits_of_bytes():
+    pages, page, heads, dim = 8200, 256, 8, 128
+    pool = dmr.KvCache.empty(pages, page, heads, dim)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for t in (pool.k, pool.v):
+        t[-3:] = torch.randn(t[-3:].shape, generator=gen, device=DEV)
+    k, v = ref.unpack(pool.k[-3:].cpu(), pool.v[-3:].cpu())
+    kb, vb = k.reshape(-1, heads, dim)[:700].double(), v.reshape(-1, heads, dim)[:700].double()
+    for n, r in ((1, 2.0 ** -8), (300, 2.0 ** -8)):
+        q = torch.randn(n, heads * dim, generator=gen, device=DEV).bfloat16()
+        out = dmr.dmr_attn_paged(pool, q, heads, dev([0, n]), dev([700]), dev([[pages - 3, pages - 2, pages - 1]]), n, 0.1)
+        want, tol = expect(q.cpu(), [(kb, vb)], [n], heads, dim, 0.1, r)
+        assert ((out.cpu().double().view(n, heads, dim) - want).abs() <= tol).all()
