@@ -281,7 +281,8 @@ dmr_status_t dmr_kv_append(const dmr_kv_cache_t *cache, const uint16_t *d_qkv, i
  * d_q and d_out are bf16 [rows][q_heads head_dim] and apart, d_block_table is [requests][table_width].  A row that sees no key is 0; rows before
  * the first request and behind the last are left as they were.  max_query is at least the largest n (rows of a request past it
  * are not computed); it chooses the kernel, so a decode step passes 1.  Scores, sums and outputs are held in fp32; of the weights
- * p_j the product with the values takes 8 bits, as the values have, and the sum that divides it the same ones.
+ * p_j the product with the values takes 16 bits where a key head has up to 32 rows of a request (max_query q_heads / kv_heads),
+ * and 8, as many as the values have, where it has more; there the sum that divides it takes the same 8.
  * Lengths past the table are read as its width, entries of the table outside the cache as its first or last page; slots
  * behind a request's last key may hold anything, NaN included.  Non-finite keys and values that a request does hold are outside
  * the contract.

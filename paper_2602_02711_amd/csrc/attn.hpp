@@ -7,12 +7,13 @@
 // out of the first product with a query per lane column and keys along the registers, which is how the second one wants its B
 // operand once the keys are taken in the matching order (key_of_row in the kernels): probabilities never leave their lane.
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace dmr {
 
 constexpr int kBlockTokens = 16;      // tokens of a cache block
-constexpr int kUnit = 64;             // keys that a kernel takes at a time
 
 struct AttnArgs {
     const uint16_t *q;
@@ -25,7 +26,7 @@ struct AttnArgs {
     float scale_log2;         // softmax scale * key scale * log2(e)
     float v_scale;
     int32_t items;            // per kv head, of the grid
-    int32_t parts;            // attn_tiles: parts of a tile's keys;  attn_few: see share_of_item, 0 for one item per request
+    int32_t parts;            // attn_tiles: parts of every tile's keys;  attn_few: as share_of_item says, 0: one item per request
 };
 
 // A request as its device arrays have it, kept inside the buffers whatever they hold.
@@ -46,6 +47,90 @@ __device__ __forceinline__ int64_t block_offset(const AttnArgs &a, const int32_t
     const int per_page = a.page_shift - 4;
     const int page = min(max(row[block >> per_page], 0), a.pages - 1);
     return (((((int64_t)page * a.kv_heads + head) << per_page) + (block & ((1 << per_page) - 1)))) * BLOCK_BYTES;
+}
+
+// The same through the scalar cache, for a block that all lanes ask for.
+template <int BLOCK_BYTES>
+__device__ __forceinline__ int64_t uniform_block_offset(const AttnArgs &a, const int32_t *row, int block, int head) {
+    typedef const __attribute__((address_space(4))) int32_t *constant_i32;
+    const int per_page = a.page_shift - 4;
+    const int page = min(max(((constant_i32)(uintptr_t)row)[block >> per_page], 0), a.pages - 1);
+    return (((((int64_t)page * a.kv_heads + head) << per_page) + (block & ((1 << per_page) - 1)))) * BLOCK_BYTES;
+}
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    auto from = [](uint32_t u, auto ctrl, auto rows) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    };
+    typedef std::integral_constant<int, 0xF> all;
+    v += from(v, std::integral_constant<int, 0x111>{}, all{});      // row_shr 1, 2, 4, 8: within rows of 16
+    v += from(v, std::integral_constant<int, 0x112>{}, all{});
+    v += from(v, std::integral_constant<int, 0x114>{}, all{});
+    v += from(v, std::integral_constant<int, 0x118>{}, all{});
+    v += from(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});      // row_bcast 15: rows 1 and 3
+    v += from(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});      // row_bcast 31: rows 2 and 3
+    return v;
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+
+// What an item of a split call does: part `part` of `parts` of the keys of rows tile `tile` of request b; its partial result, and
+// those of the tile's other parts, are at items first_item .. first_item + parts - 1.  b < 0: nothing.
+struct Share {
+    int b, tile, part, parts, first_item;
+    Request rq;
+};
+
+// Item -> tile where every tile has a.parts parts: request b has ceil(n G / tile_rows) tiles.
+__device__ __forceinline__ Share share_of_tile(const AttnArgs &a, int tile, int tile_rows, int lane) {
+    for (int base = 0; base < a.requests; base += 64) {
+        const int i = base + lane;
+        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
+        const uint32_t tiles = (uint32_t)((r.n * a.G + tile_rows - 1) / tile_rows), upto = wave_scan(tiles);
+        const uint64_t above = __ballot((int)upto > tile);
+        if (above) {
+            const int l = __builtin_ctzll(above);
+            return Share{base + l, tile - (int)lane_value(upto - tiles, l), 0, a.parts, 0,
+                         Request{(int)lane_value(r.first, l), (int)lane_value(r.n, l), (int)lane_value(r.keys, l)}};
+        }
+        tile -= (int)lane_value(upto, 63);
+    }
+    return Share{-1, 0, 0, 0, 0, Request{0, 0, 0}};
+}
+
+// One tile per request, its keys in as many parts as its length asks for.  With U units of UNIT keys in the whole batch, parts of
+// C = max(kMinUnits, ceil(U / a.parts)) units at most make no more than a.parts + requests items, whatever the lengths: each
+// workgroup forms the same sums from the lengths on the device, so that a captured call splits the lengths of its replay and a
+// ragged batch's longest request decides nothing.  `item` is an item's number, or with BY_REQUEST a request's.
+constexpr int kMinUnits = 4;      // a unit for each wave of a workgroup
+template <int UNIT, bool BY_REQUEST>
+__device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int lane) {
+    uint64_t total = 0;
+    auto units_of = [](const Request &r) { return (uint32_t)(r.n > 0 ? (r.keys + UNIT - 1) / UNIT : 0); };
+    for (int base = 0; base < a.requests; base += 64) {
+        const int i = base + lane;
+        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
+        total += lane_value(wave_scan(units_of(r)), 63);
+    }
+    const uint32_t C = (uint32_t)std::max<uint64_t>(kMinUnits, (total + (uint32_t)a.parts - 1) / (uint32_t)a.parts);
+    int before = 0;
+    for (int base = 0; base < a.requests; base += 64) {
+        const int i = base + lane;
+        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
+        const uint32_t items = r.n > 0 ? std::max(1u, (units_of(r) + C - 1) / C) : 0u, upto = wave_scan(items);
+        int l = item - base;
+        if constexpr (!BY_REQUEST) {
+            const uint64_t above = __ballot(before + (int)upto > item);
+            l = above ? __builtin_ctzll(above) : 64;
+        }
+        if (l < 64) {
+            const int first = before + (int)lane_value(upto - items, l), parts = (int)lane_value(items, l);
+            return Share{base + l, 0, BY_REQUEST ? 0 : item - first, parts, first,
+                         Request{(int)lane_value(r.first, l), (int)lane_value(r.n, l), (int)lane_value(r.keys, l)}};
+        }
+        before += (int)lane_value(upto, 63);
+    }
+    return Share{-1, 0, 0, 0, 0, Request{0, 0, 0}};
 }
 
 // Eight e4m3 bytes to eight bf16 (exact).
@@ -79,14 +164,18 @@ hipError_t launch_kv_append(const CacheView &c, const uint16_t *qkv, int64_t row
 
 // How a call of dmr_attn_paged is split, from what the host knows: pure arithmetic, the same for the workspace query and the launch.
 struct AttnPlan {
+    bool few;                 // attn_few: one tile of 16 or 32 rows per request
     int tile_rows;            // (token, query head) rows of a tile
     int64_t items;            // workgroups per kv head
     int parts;                // AttnArgs::parts
     bool split;               // several items may belong to one tile: partial results, joined by a second kernel
 };
+constexpr int few_unit(bool e4m3) { return e4m3 ? 64 : 32; }      // keys that a wave of attn_few takes at a time
 AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query);
 inline size_t attn_part_floats(const AttnPlan &p, int kv_heads, int D) { return (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows * (size_t)D; }
 hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream);
-hipError_t launch_attn_join(const AttnArgs &a, int tile_rows, int D, hipStream_t stream);
+hipError_t launch_attn_few(const AttnArgs &a, const AttnPlan &p, int D, bool e4m3, hipStream_t stream);
+// Joins the parts that a split call left; `rows` of a tile at most.
+hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, bool e4m3, hipStream_t stream);
 
 }  // namespace dmr

@@ -133,9 +133,10 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
                           (int32_t)cache->pages, view.page_shift, scale * view.k_scale * 1.44269504088896340736f, view.v_scale,
                           (int32_t)plan.items, plan.parts};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t e = dmr::launch_attn_tiles(a, view.D, view.e4m3, s);
+    const hipError_t e = plan.few ? dmr::launch_attn_few(a, plan, view.D, view.e4m3, s) : dmr::launch_attn_tiles(a, view.D, view.e4m3, s);
     if (e != hipSuccess || !plan.split) return hip_status(e);
-    return hip_status(dmr::launch_attn_join(a, plan.tile_rows, view.D, s));
+    return hip_status(dmr::launch_attn_join(a, plan, (int)std::min<int64_t>(std::min(max_query, rows) * a.G, plan.tile_rows), view.D,
+                                            view.e4m3, s));
 }
 
 }  // extern "C"

@@ -12,6 +12,7 @@ namespace dmr {
 namespace {
 
 constexpr int kRows = 128;      // of a tile
+constexpr int kUnit = 64;       // keys staged at a time
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256, 1) void attn_tiles_kernel(AttnArgs a) {
@@ -21,34 +22,13 @@ __global__ __launch_bounds__(256, 1) void attn_tiles_kernel(AttnArgs a) {
     __shared__ __align__(16) uint8_t sk[4 * BLOCK], sv[4 * BLOCK];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, h = lane >> 5;
     const int head = (int)blockIdx.x % a.kv_heads, item = (int)blockIdx.x / a.kv_heads;
-    int tile = item / a.parts;
-    const int part = item - tile * a.parts;
-
-    // which request has this tile
-    int b = -1;
-    Request rq{0, 0, 0};
-    for (int base = 0; base < a.requests; base += 64) {
-        const int i = base + lane;
-        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
-        const int64_t tiles = ((int64_t)r.n * a.G + kRows - 1) / kRows;
-        int64_t upto = tiles;
-        for (int d = 1; d < 64; d *= 2) {
-            const int64_t u = __shfl_up(upto, d);
-            if (lane >= d) upto += u;
-        }
-        const uint64_t above = __ballot(upto > tile);
-        if (above) {
-            const int l = __builtin_ctzll(above);
-            tile -= (int)__shfl(upto - tiles, l);
-            b = base + l;
-            rq = Request{__shfl(r.first, l), __shfl(r.n, l), __shfl(r.keys, l)};
-            break;
-        }
-        tile -= (int)__shfl(upto, 63);
-    }
-    if (b < 0) return;
+    const int part = item % a.parts;
+    const Share sh = share_of_tile(a, item / a.parts, kRows, lane);
+    if (sh.b < 0) return;
+    const Request rq = sh.rq;
+    const int tile = sh.tile;
     const int rows = rq.n * a.G, row0 = tile * kRows;
-    const int32_t *pages = a.table + (int64_t)b * a.width;
+    const int32_t *pages = a.table + (int64_t)sh.b * a.width;
     // this lane's query; rows past the last repeat it
     const int row = min(row0 + 32 * wave + col, rows - 1), token = row / a.G, qh = head * a.G + row % a.G;
     const int64_t q_at = ((int64_t)(rq.first + token) * a.q_heads + qh) * D;
@@ -165,68 +145,7 @@ __global__ __launch_bounds__(256, 1) void attn_tiles_kernel(AttnArgs a) {
         }
 }
 
-// Parts of a tile's keys joined: out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j, M the largest m_j.  A wave has a row.
-template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_rows) {
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int head = (int)blockIdx.x % a.kv_heads;
-    int tile = (int)blockIdx.x / a.kv_heads;
-    const int slot_tile = tile;
-    int b = -1;
-    Request rq{0, 0, 0};
-    for (int base = 0; base < a.requests; base += 64) {
-        const int i = base + lane;
-        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
-        const int64_t tiles = ((int64_t)r.n * a.G + tile_rows - 1) / tile_rows;
-        int64_t upto = tiles;
-        for (int d = 1; d < 64; d *= 2) {
-            const int64_t u = __shfl_up(upto, d);
-            if (lane >= d) upto += u;
-        }
-        const uint64_t above = __ballot(upto > tile);
-        if (above) {
-            const int l = __builtin_ctzll(above);
-            tile -= (int)__shfl(upto - tiles, l);
-            b = base + l;
-            rq = Request{__shfl(r.first, l), __shfl(r.n, l), __shfl(r.keys, l)};
-            break;
-        }
-        tile -= (int)__shfl(upto, 63);
-    }
-    if (b < 0) return;
-    const int rows = rq.n * a.G, in_tile = (int)blockIdx.y * 4 + wave, row = tile * tile_rows + in_tile;
-    if (row >= rows) return;
-    const int64_t slot0 = ((int64_t)slot_tile * a.parts * a.kv_heads + head) * tile_rows + in_tile, step = (int64_t)a.kv_heads * tile_rows;
-    float M = kNoKey;
-    for (int j = 0; j < a.parts; ++j) M = fmaxf(M, a.ml[slot0 + j * step].x);
-    float L = 0.f, acc[D / 64] = {};
-    for (int j = 0; j < a.parts; ++j) {
-        const float2 ml = a.ml[slot0 + j * step];
-        const float w = exp2_fast(ml.x - M);
-        L += w * ml.y;
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) acc[e] += w * a.part[(slot0 + j * step) * D + lane + 64 * e];
-    }
-    const int64_t at = ((int64_t)(rq.first + row / a.G) * a.q_heads + head * a.G + row % a.G) * D;
-    const float r = L > 0.f ? a.v_scale / L : 0.f;
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) a.out[at + lane + 64 * e] = f32_to_bf16(acc[e] * r);
-}
-
 }  // namespace
-
-// Tiles that `rows` rows of `requests` requests can make, each of at most max_query.
-AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query) {
-    const int64_t G = q_heads / kv_heads;
-    AttnPlan p;
-    p.tile_rows = kRows;
-    const int64_t by_request = requests * ((std::min(max_query, rows) * G + kRows - 1) / kRows), by_row = rows * G / kRows + requests;
-    const int64_t tiles = std::min(by_request, by_row);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(32, 512 / std::max<int64_t>(1, tiles * kv_heads)));
-    p.items = tiles * p.parts;
-    p.split = p.parts > 1;
-    return p;
-}
 
 hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream) {
     const dim3 grid((unsigned)(a.items * a.kv_heads));
@@ -236,13 +155,6 @@ hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t st
     } else {
         if (e4m3) go(attn_tiles_kernel<128, true>); else go(attn_tiles_kernel<128, false>);
     }
-    return hipGetLastError();
-}
-
-hipError_t launch_attn_join(const AttnArgs &a, int tile_rows, int D, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.items / a.parts * a.kv_heads), (unsigned)(tile_rows / 4));
-    if (D == 64) hipLaunchKernelGGL(attn_join_kernel<64>, grid, dim3(256), 0, stream, a, tile_rows);
-    else hipLaunchKernelGGL(attn_join_kernel<128>, grid, dim3(256), 0, stream, a, tile_rows);
     return hipGetLastError();
 }
 

@@ -15,20 +15,10 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kInLaunchRows = 4096;
 constexpr int32_t kRefused = INT32_MIN;
 
-// Inclusive sum over the wave of values whose sum over 64 lanes fits 32 bits.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint32_t u = __shfl_up(v, d);
-        if (lane >= d) v += u;
-    }
-    return v;
-}
-
-// Inclusive sum over the workgroup on top of `carry`, which moves on to the total.
+// Inclusive sum over the workgroup on top of `carry`, which moves on to the total.  A wave's own sum fits 32 bits.
 __device__ __forceinline__ int64_t block_scan(uint32_t v, int64_t &carry, uint32_t *sums) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t in_wave = wave_scan(v, lane);
+    const uint32_t in_wave = wave_scan(v);
     __syncthreads();                       // `sums` of the scan before
     if (lane == 63) sums[wave] = in_wave;
     __syncthreads();

@@ -2,9 +2,9 @@
 
 Tolerance of an element, with A = sum p |v| / sum p.  A score is off by at most (dim + 4) 2^-24 of scale sum |q k| (products of bf16 are
 exact in fp32, their sum is not; then the scale, and in the exponent's log2 units), so a weight by e = (dim + 16) 2^-23 (1 + that
-sum) of itself, exponential included.  The kernel rounds each weight to 8 bits, r = 2^-8, and divides by the sum of these:
-numerator and denominator move by (r + e) of A and of the result.  The sums' own roundings, at most keys 2^-24 of A, stand in a
-factor of 2 on e.  Then one rounding to bf16, 2^-8 of the result."""
+sum) of itself, exponential included.  The kernel for many rows rounds each weight to 8 bits, r = 2^-8, and divides by the sum
+of these, the one for few (up to 32 to a key head) takes 16, r = 2^-16: numerator and denominator move by (r + e) of A and of the
+result.  The sums' own roundings, at most keys 2^-24 of A, stand in a factor of 2 on e.  Then one rounding to bf16, 2^-8 of the result."""
 import numpy as np
 import pytest
 import torch
@@ -52,6 +52,10 @@ def build(seed, news, lens, heads, kv_heads, dim, page, cache, sharp=2.0, extra_
     return pool, q, keys, table
 
 
+def rounding_of_weights(most, heads, kv_heads):
+    return 2.0 ** -16 if most * (heads // kv_heads) <= 32 else 2.0 ** -8
+
+
 def expect(q, keys, news, heads, dim, scale, r):
     out, tol, at = [], [], 0
     for (kb, vb), n in zip(keys, news):
@@ -76,7 +80,7 @@ def check(seed, news, lens, heads, kv_heads, dim, page, cache, sharp=2.0, pad=3,
     assert (ws[max(need, 16):] == 0xFF).all()
     assert (out[rows:] == SENTINEL).all()
     # a request of no keys sees none of its rows; one of fewer keys than rows, only the last
-    want, tol = expect(q, keys, news, heads, dim, scale, 2.0 ** -8)
+    want, tol = expect(q, keys, news, heads, dim, scale, rounding_of_weights(min(most, rows + pad), heads, kv_heads))
     got = out[:rows].cpu().double().view(rows, heads, dim)
     assert torch.isfinite(got).all()
     over = (got - want).abs() - tol
@@ -194,7 +198,7 @@ def test_pages_shared_by_requests():
     table[1, :2] = table[0, :2]
     keys[1] = tuple(torch.cat([a[:128], b[128:]]) for a, b in zip(keys[0], keys[1]))
     out = dmr.dmr_attn_paged(pool, q.to(DEV), 4, dev([0, 1, 2]), dev([200, 130]), dev(table), 1, 0.125)
-    want, tol = expect(q, keys, [1, 1], 4, 64, 0.125, 2.0 ** -8)
+    want, tol = expect(q, keys, [1, 1], 4, 64, 0.125, 2.0 ** -16)
     assert ((out.cpu().double().view(2, 4, 64) - want).abs() <= tol).all()
 
 
@@ -205,7 +209,7 @@ def test_entries_and_lengths_out_of_range_stay_in_the_cache():
         t.nan_to_num_(0.0)
     table[1] = [10 ** 6, -5, 2 ** 31 - 1, -2 ** 31, 77][:table.shape[1]]
     out = dmr.dmr_attn_paged(pool, q.to(DEV), 4, dev([0, 1, 2, 3]), dev([200, 2 ** 31 - 1, 90]), dev(table), 1, 0.125)
-    want, tol = expect(q, keys, [1, 1, 1], 4, 64, 0.125, 2.0 ** -8)
+    want, tol = expect(q, keys, [1, 1, 1], 4, 64, 0.125, 2.0 ** -16)
     ok = (out.cpu().double().view(3, 4, 64) - want).abs() <= tol
     assert ok[0].all() and ok[2].all() and torch.isfinite(out).all()
 
@@ -218,7 +222,7 @@ def test_cache_past_32_bits_of_bytes():
         t[-3:] = torch.randn(t[-3:].shape, generator=gen, device=DEV)
     k, v = ref.unpack(pool.k[-3:].cpu(), pool.v[-3:].cpu())
     kb, vb = k.reshape(-1, heads, dim)[:700].double(), v.reshape(-1, heads, dim)[:700].double()
-    for n, r in ((1, 2.0 ** -8), (300, 2.0 ** -8)):
+    for n, r in ((1, 2.0 ** -16), (300, 2.0 ** -8)):
         q = torch.randn(n, heads * dim, generator=gen, device=DEV).bfloat16()
         out = dmr.dmr_attn_paged(pool, q, heads, dev([0, n]), dev([700]), dev([[pages - 3, pages - 2, pages - 1]]), n, 0.1)
         want, tol = expect(q.cpu(), [(kb, vb)], [n], heads, dim, 0.1, r)
