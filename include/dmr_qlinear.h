@@ -278,7 +278,7 @@ dmr_status_t dmr_kv_append(const dmr_kv_cache_t *cache, const uint16_t *d_qkv, i
  * d_query_start[b] on, the last n of its d_kv_lens[b] keys (dmr_kv_append has written them): its row i sees the keys
  * 0 .. d_kv_lens[b] - n + i, and query head h the keys of head h / (q_heads / kv_heads):
  *   out[i][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * (q[i][h] . k_j))
- * d_q and d_out are bf16 [rows][q_heads head_dim] and apart, d_block_table is [requests][table_width].  A row that sees no key is 0; rows before
+ * scale is positive.  d_q and d_out are bf16 [rows][q_heads head_dim] and apart, d_block_table is [requests][table_width].  A row that sees no key is 0; rows before
  * the first request and behind the last are left as they were.  max_query is at least the largest n (rows of a request past it
  * are not computed); it chooses the kernel, so a decode step passes 1.  Scores, sums and outputs are held in fp32; of the weights
  * p_j the product with the values takes 16 bits where a key head has up to 32 rows of a request (max_query q_heads / kv_heads),

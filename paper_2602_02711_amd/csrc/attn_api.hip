@@ -117,7 +117,8 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
     if (rows < 0 || rows > kMaxRows || requests < 0 || requests > kMaxRequests || table_width <= 0 ||
         table_width > INT32_MAX / cache->page_tokens || max_query < 0 || rows * (int64_t)(q_heads / cache->kv_heads) > INT32_MAX)
         return DMR_ERR_SHAPE;
-    if (!std::isfinite(scale)) return DMR_ERR_UNSUPPORTED;
+    const float scale_log2 = scale * view.k_scale * 1.44269504088896340736f;
+    if (!(scale > 0.f) || !std::isnormal(scale_log2)) return DMR_ERR_UNSUPPORTED;
     if (rows == 0 || requests == 0 || max_query == 0) return DMR_OK;
     if (!all_there(cache->d_k, cache->d_v, d_q, d_query_start, d_kv_lens, d_block_table, d_out)) return DMR_ERR_NULL;
     if (!all_aligned(cache->d_k, cache->d_v, d_q, d_out, d_ws) || !words_aligned(d_query_start, d_kv_lens, d_block_table)) return DMR_ERR_ALIGN;
@@ -130,7 +131,7 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
                           plan.split ? static_cast<float *>(d_ws) : nullptr,
                           plan.split ? reinterpret_cast<float2 *>(static_cast<uint8_t *>(d_ws) + part) : nullptr,
                           (int32_t)rows, (int32_t)requests, (int32_t)table_width, q_heads, cache->kv_heads, q_heads / cache->kv_heads,
-                          (int32_t)cache->pages, view.page_shift, scale * view.k_scale * 1.44269504088896340736f, view.v_scale,
+                          (int32_t)cache->pages, view.page_shift, scale_log2, view.v_scale,
                           (int32_t)plan.items, plan.parts};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = plan.few ? dmr::launch_attn_few(a, plan, view.D, view.e4m3, s) : dmr::launch_attn_tiles(a, view.D, view.e4m3, s);

@@ -3,9 +3,13 @@
 //
 // S^T = K Q^T on 32 x 32 x 16 MFMAs leaves lane l with the scores of query l % 32 for 16 keys of each 32, so the running maximum and
 // sum are per-lane numbers, and the weights, rounded to bf16 in place, are the B operand of O^T += V^T P^T, whose columns are
-// the queries again.  Row r of a score tile is key key_of_row(r): the order in which lane half l / 32 then holds 8 consecutive
-// keys of each 16, as the pieces of the value pool do.
+// the queries again.  Row r of a score tile is key 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4 of block r / 16: the order in which lane half
+// l / 32 then holds 8 consecutive keys of each 16, as the pieces of the value pool do.
+//
+// The keys and values of the next 64 arrive while these are worked on: bf16 ones by loads into the other half of the buffer, e4m3
+// ones through registers, where a thread makes them bf16 once for all four waves.  One barrier for each 64 keys.
 #include "attn.hpp"
+#include "lds_loads.hpp"
 
 namespace dmr {
 
@@ -13,27 +17,32 @@ namespace {
 
 constexpr int kRows = 128;      // of a tile
 constexpr int kUnit = 64;       // keys staged at a time
+constexpr float kSlack = 8.f;   // the reference of the exponents may lag the largest score by 2^8
+
+typedef __attribute__((ext_vector_type(2))) __bf16 pair_bf16;
 
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256, 1) void attn_tiles_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     constexpr int BLOCK = 16 * D * 2;                         // bytes of a block as bf16
     constexpr int SRC = E4M3 ? 16 * D : 16 * D * 2;           // and in the cache
-    constexpr int PIECES = SRC / 16;                          // of 16 bytes
-    __shared__ __align__(16) uint8_t sk[4 * BLOCK], sv[4 * BLOCK];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, h = lane >> 5;
+    constexpr int STAGE = 4 * BLOCK;                          // keys of a unit, and values
+    __shared__ __align__(16) uint8_t lds[4 * STAGE];          // [2][keys, values]
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int head = (int)blockIdx.x % a.kv_heads, item = (int)blockIdx.x / a.kv_heads;
     const int part = item % a.parts;
     const Share sh = share_of_tile(a, item / a.parts, kRows, lane);
     if (sh.b < 0) return;
     const Request rq = sh.rq;
-    const int tile = sh.tile;
-    const int rows = rq.n * a.G, row0 = tile * kRows;
+    const int rows = rq.n * a.G, row0 = sh.tile * kRows;
     const int32_t *pages = a.table + (int64_t)sh.b * a.width;
     // this lane's query; rows past the last repeat it
     const int row = min(row0 + 32 * wave + col, rows - 1), token = row / a.G, qh = head * a.G + row % a.G;
     const int64_t q_at = ((int64_t)(rq.first + token) * a.q_heads + qh) * D;
     const int seen = rq.keys - rq.n + token + 1;              // keys this lane's query sees
-    const int most = rq.keys - rq.n + min(row0 + kRows - 1, rows - 1) / a.G + 1;      // and the tile's last one
+    auto seen_by = [&](int r) { return rq.keys - rq.n + min(r, rows - 1) / a.G + 1; };
+    const int most = seen_by(row0 + kRows - 1);               // the tile's last row
+    const int wave_least = __builtin_amdgcn_readfirstlane(seen_by(row0 + 32 * wave));
+    const int wave_most = __builtin_amdgcn_readfirstlane(row0 + 32 * wave < rows ? seen_by(row0 + 32 * wave + 31) : 0);
     const int units = most > 0 ? (most + kUnit - 1) / kUnit : 0;
     const int u0 = (int)((int64_t)units * part / a.parts), u1 = (int)((int64_t)units * (part + 1) / a.parts);
 
@@ -47,79 +56,130 @@ __global__ __launch_bounds__(256, 1) void attn_tiles_kernel(AttnArgs a) {
     const int last_block = (rq.keys - 1) >> 4;
     const int key_row = 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), key_block = col >> 4;
 
-    for (int u = u0; u < u1; ++u) {
-        __syncthreads();
+    // staging: with bf16, load i of a block is 4 KB (2 KB where D is 64: two waves' worth each); e4m3 pieces in registers
+    constexpr int CHUNKS = E4M3 ? 4 * SRC / 4096 : 0;         // 16-byte pieces of a unit's keys, and values, for each thread
+    u32x4_t hk[CHUNKS ? CHUNKS : 1], hv[CHUNKS ? CHUNKS : 1];
+    auto request = [&](int u, int buf) {
+        if constexpr (E4M3) {
 #pragma unroll
-        for (int blk = 0; blk < 4; ++blk) {
-            const int64_t src = block_offset<SRC>(a, pages, min(4 * u + blk, last_block), head);
-            for (int p = tid; p < PIECES; p += 256) {
-                const uint4 kp = *reinterpret_cast<const uint4 *>(a.k + src + 16 * p);
-                const uint4 vp = *reinterpret_cast<const uint4 *>(a.v + src + 16 * p);
-                if constexpr (E4M3) {
-                    uint8_t *dk = sk + blk * BLOCK + (p >> 4) * 512 + (p & 15) * 16;      // pieces 2 p' and 2 p' + 1 of a token
-                    *reinterpret_cast<uint4 *>(dk) = bf16_of_e4m3(kp.x, kp.y);
-                    *reinterpret_cast<uint4 *>(dk + 256) = bf16_of_e4m3(kp.z, kp.w);
-                    uint8_t *dv = sv + blk * BLOCK + p * 16;                              // tokens 0 .. 7 and 8 .. 15 of an element
-                    *reinterpret_cast<uint4 *>(dv) = bf16_of_e4m3(vp.x, vp.y);
-                    *reinterpret_cast<uint4 *>(dv + D * 16) = bf16_of_e4m3(vp.z, vp.w);
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int piece = i * 256 + tid, blk = piece / (SRC / 16), p = piece % (SRC / 16);
+                const int64_t src = block_offset<SRC>(a, pages, min(4 * u + blk, last_block), head) + 16 * p;
+                hk[i] = *reinterpret_cast<const u32x4_t *>(a.k + src);
+                hv[i] = *reinterpret_cast<const u32x4_t *>(a.v + src);
+            }
+        } else {
+            uint8_t *dst = lds + buf * (2 * STAGE);
+#pragma unroll
+            for (int blk = 0; blk < 4; ++blk) {
+                const int64_t src = uniform_block_offset<SRC>(a, pages, min(4 * u + blk, last_block), head);
+                if constexpr (D == 128) {
+                    load16_to_lds(a.k + src, BLOCK, dst + blk * BLOCK + wave * 1024, (uint32_t)(tid * 16), 0);
+                    load16_to_lds(a.v + src, BLOCK, dst + STAGE + blk * BLOCK + wave * 1024, (uint32_t)(tid * 16), 0);
                 } else {
-                    *reinterpret_cast<uint4 *>(sk + blk * BLOCK + 16 * p) = kp;
-                    *reinterpret_cast<uint4 *>(sv + blk * BLOCK + 16 * p) = vp;
+                    // half of a block's keys and half of its values to each pair of waves
+                    const uint8_t *from = wave & 2 ? a.v : a.k;
+                    uint8_t *to = dst + (wave & 2 ? STAGE : 0) + blk * BLOCK + (wave & 1) * 1024;
+                    load16_to_lds(from + src, BLOCK, to, (uint32_t)((tid & 127) * 16), 0);
                 }
             }
         }
-        __syncthreads();
+    };
+    auto arrive = [&](int buf) {
+        if constexpr (E4M3) {
+            uint8_t *dst = lds + buf * (2 * STAGE);
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int piece = i * 256 + tid, blk = piece / (SRC / 16), p = piece % (SRC / 16);
+                uint8_t *dk = dst + blk * BLOCK + (p >> 4) * 512 + (p & 15) * 16;      // pieces 2 p' and 2 p' + 1 of a token
+                *reinterpret_cast<uint4 *>(dk) = bf16_of_e4m3(hk[i][0], hk[i][1]);
+                *reinterpret_cast<uint4 *>(dk + 256) = bf16_of_e4m3(hk[i][2], hk[i][3]);
+                uint8_t *dv = dst + STAGE + blk * BLOCK + p * 16;                      // tokens 0 .. 7 and 8 .. 15 of an element
+                *reinterpret_cast<uint4 *>(dv) = bf16_of_e4m3(hv[i][0], hv[i][1]);
+                *reinterpret_cast<uint4 *>(dv + D * 16) = bf16_of_e4m3(hv[i][2], hv[i][3]);
+            }
+            wait_lds();
+        } else {
+            wait_loads<0>();
+        }
+        bare_barrier();
+    };
+
+    // EDGE: some key of the unit is not seen by some row of the wave, or lies behind the request's last
+    auto unit = [&](int first, int buf, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;
+        const uint8_t *sk = lds + buf * (2 * STAGE) + key_block * BLOCK + h * 256 + key_row * 16;
+        const uint8_t *sv = lds + buf * (2 * STAGE) + STAGE + h * (D * 16) + col * 16;
+        f32x16 s[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int base = u * kUnit + 32 * half;
-            f32x16 s = f32x16{};
+            Frag k[D / 16];
+            read_frags<D / 16, 512>(sk + 2 * half * BLOCK, sk + 2 * half * BLOCK, k);
+            s[half] = f32x16{};
 #pragma unroll
-            for (int st = 0; st < D / 16; ++st) {
-                Frag k;
-                k.u = *reinterpret_cast<const uint4 *>(sk + (2 * half + key_block) * BLOCK + (2 * st + h) * 256 + key_row * 16);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[st].v, s, 0, 0, 0);
-            }
-            // register i is key base + 16 (i / 8) + 8 h + i % 8
-            float x[16], top = kNoKey;
+            for (int st = 0; st < D / 16; ++st) s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[st].v, q[st].v, s[half], 0, 0, 0);
+        }
+        // register i of half is key first + 32 half + 16 (i / 8) + 8 h + i % 8
+        if constexpr (EDGE) {
+            const int left = seen - first - 8 * h;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = base + 16 * (i >> 3) + 8 * h + (i & 7);
-                x[i] = key < seen ? s[i] * a.scale_log2 : -INFINITY;
-                top = fmaxf(top, x[i]);
-            }
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m_new = fmaxf(m, top), fade = exp2_fast(m - m_new);
-            m = m_new;
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[half][i] = 32 * half + 16 * (i >> 3) + (i & 7) < left ? s[half][i] : -INFINITY;
+        }
+        float top = kNoKey;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(s[half][i], s[half][i + 1]));
+        top *= a.scale_log2;
+        // only then is the reference moved, and with it what was summed so far
+        if (__any(top > m + kSlack)) {
+            const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), fade = exp2_fast(m - to);
+            m = to;
             l *= fade;
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t)
+            for (int t = 0; t < D / 32; ++t) o[t] *= fade;
+        }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] *= fade;
+        for (int half = 0; half < 2; ++half) {
             Frag p[2];
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float e0 = exp2_fast(x[i] - m), e1 = exp2_fast(x[i + 1] - m);
+                const float e0 = exp2_fast(fmaf(s[half][i], a.scale_log2, -m)), e1 = exp2_fast(fmaf(s[half][i + 1], a.scale_log2, -m));
                 const uint32_t w = pack_bf16x2(e0, e1);
                 p[i >> 3].w[(i & 7) >> 1] = w;
-                l += __uint_as_float(w << 16) + __uint_as_float(w & 0xFFFF0000u);
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_bf16, w), __builtin_bit_cast(pair_bf16, 0x3F803F80u), l, false);
             }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                // values of slots behind the last key may hold anything: 0 x NaN is NaN
-                const int left = rq.keys - (base + 16 * st + 8 * h);
-                uint32_t mask[4];
+                Frag v[D / 32];
+                read_frags<D / 32, 512>(sv + (2 * half + st) * BLOCK, sv + (2 * half + st) * BLOCK, v);
+                if constexpr (EDGE) {      // values of slots behind the last key may hold anything, and 0 x NaN is NaN
+                    const int left = rq.keys - (first + 32 * half + 16 * st + 8 * h);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) mask[w] = (2 * w < left ? 0xFFFFu : 0u) | (2 * w + 1 < left ? 0xFFFF0000u : 0u);
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t keep = (2 * w < left ? 0xFFFFu : 0u) | (2 * w + 1 < left ? 0xFFFF0000u : 0u);
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    Frag v;
-                    v.u = *reinterpret_cast<const uint4 *>(sv + (2 * half + st) * BLOCK + h * (D * 16) + (32 * t + col) * 16);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v.w[w] &= mask[w];
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p[st].v, o[t], 0, 0, 0);
+                        for (int t = 0; t < D / 32; ++t) v[t].w[w] &= keep;
+                    }
                 }
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[t].v, p[st].v, o[t], 0, 0, 0);
             }
         }
+    };
+
+    if (u0 < u1) {
+        request(u0, 0);
+        arrive(0);
+    }
+    for (int u = u0; u < u1; ++u) {
+        const int buf = (u - u0) & 1, first = u * kUnit;
+        if (u + 1 < u1) request(u + 1, buf ^ 1);
+        if (first + kUnit <= wave_least) unit(first, buf, std::false_type{});
+        else if (first < wave_most) unit(first, buf, std::true_type{});
+        if (u + 1 < u1) arrive(buf ^ 1);
     }
     l += __shfl_xor(l, 32);
     if (row0 + 32 * wave + col >= rows) return;

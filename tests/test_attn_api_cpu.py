@@ -85,7 +85,8 @@ def test_attend(lib):
     S, U, N, A = b.DMR_ERR_SHAPE, b.DMR_ERR_UNSUPPORTED, b.DMR_ERR_NULL, b.DMR_ERR_ALIGN
     for bad, want in ((dict(rows=-1), S), (dict(rows=2 ** 22 + 1), S), (dict(requests=-1), S), (dict(requests=2 ** 20 + 1), S), (dict(width=0), S),
                       (dict(width=2 ** 26), S), (dict(most=-1), S), (dict(heads=33), S), (dict(heads=-8), S), (dict(scale=float("inf")), U),
-                      (dict(scale=float("nan")), U), (dict(q=None), N), (dict(start=None), N), (dict(lens=None), N), (dict(table=None), N),
+                      (dict(scale=float("nan")), U), (dict(scale=0.0), U),
+                      (dict(scale=-0.1), U), (dict(scale=1e-40), U), (dict(q=None), N), (dict(start=None), N), (dict(lens=None), N), (dict(table=None), N),
                       (dict(out=None), N), (dict(q=FAKE + 8), A), (dict(out=FAKE + 2), A), (dict(ws=FAKE + 8), A), (dict(start=FAKE + 2), A),
                       (dict(lens=FAKE + 1), A), (dict(table=FAKE + 3), A), (dict(rows=0), b.DMR_OK), (dict(requests=0), b.DMR_OK),
                       (dict(most=0), b.DMR_OK)):
