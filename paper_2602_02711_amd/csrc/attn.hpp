@@ -98,21 +98,29 @@ __device__ __forceinline__ Share share_of_tile(const AttnArgs &a, int tile, int 
     return Share{-1, 0, 0, 0, 0, Request{0, 0, 0}};
 }
 
-// One tile per request, its keys in as many parts as its length asks for.  With U units of UNIT keys in the whole batch, parts of
-// C = max(kMinUnits, ceil(U / a.parts)) units at most make no more than a.parts + requests items, whatever the lengths: each
-// workgroup forms the same sums from the lengths on the device, so that a captured call splits the lengths of its replay and a
-// ragged batch's longest request decides nothing.  `item` is an item's number, or with BY_REQUEST a request's.
+// One tile per request, its keys in as many parts as its length asks for.  With U units of UNIT keys in the whole batch and
+// C = max(kMinUnits, ceil(U / a.parts)), a request of u units has ceil(u / C) parts, one at least: no more than a.parts + requests
+// items, whatever the lengths.  A batch that gives every CU a workgroup and whose longest request is no longer than 3 / 2 of the mean
+// is not split.  Each workgroup forms the same sums from the lengths on the device, so that a captured call splits the lengths
+// of its replay and a ragged batch's longest request decides nothing.  `item` is an item's number, or with BY_REQUEST a request's.
 constexpr int kMinUnits = 4;      // a unit for each wave of a workgroup
 template <int UNIT, bool BY_REQUEST>
 __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int lane) {
     uint64_t total = 0;
+    uint32_t longest = 0, some = 0;
     auto units_of = [](const Request &r) { return (uint32_t)(r.n > 0 ? (r.keys + UNIT - 1) / UNIT : 0); };
     for (int base = 0; base < a.requests; base += 64) {
         const int i = base + lane;
         const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
-        total += lane_value(wave_scan(units_of(r)), 63);
+        const uint32_t u = units_of(r);
+        total += lane_value(wave_scan(u), 63);
+        longest = std::max(longest, u);
+        some += (uint32_t)__popcll(__ballot(r.n > 0));
     }
-    const uint32_t C = (uint32_t)std::max<uint64_t>(kMinUnits, (total + (uint32_t)a.parts - 1) / (uint32_t)a.parts);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) longest = std::max(longest, (uint32_t)__shfl_xor((int)longest, d));
+    uint32_t C = (uint32_t)std::max<uint64_t>(kMinUnits, (total + (uint32_t)a.parts - 1) / (uint32_t)a.parts);
+    if (some * (uint32_t)a.kv_heads >= (uint32_t)kCus && (uint64_t)longest * some * 2 <= total * 3) C = std::max(C, longest);
     int before = 0;
     for (int base = 0; base < a.requests; base += 64) {
         const int i = base + lane;
@@ -171,7 +179,7 @@ struct AttnPlan {
     bool split;               // several items may belong to one tile: partial results, joined by a second kernel
 };
 constexpr int few_unit(bool e4m3) { return e4m3 ? 64 : 32; }      // keys that a wave of attn_few takes at a time
-AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query);
+AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query, int64_t capacity, bool e4m3);
 inline size_t attn_part_floats(const AttnPlan &p, int kv_heads, int D) { return (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows * (size_t)D; }
 hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream);
 hipError_t launch_attn_few(const AttnArgs &a, const AttnPlan &p, int D, bool e4m3, hipStream_t stream);

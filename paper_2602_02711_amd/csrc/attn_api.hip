@@ -6,6 +6,7 @@
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxRequests = int64_t(1) << 20;
+constexpr int32_t kMaxHeads = 4096;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 template <typename... P>
@@ -26,7 +27,7 @@ int page_shift_of(int32_t page_tokens) {
 
 // Shape of a cache: DMR_OK, or what is wrong with it.
 dmr_status_t check_layout(int32_t page_tokens, int32_t kv_heads, int32_t head_dim, dmr_kv_type_t type) {
-    if (page_tokens <= 0 || kv_heads <= 0 || kv_heads > 65536 || head_dim <= 0) return DMR_ERR_SHAPE;
+    if (page_tokens <= 0 || kv_heads <= 0 || kv_heads > kMaxHeads || head_dim <= 0) return DMR_ERR_SHAPE;
     if (page_shift_of(page_tokens) < 0 || (head_dim != 64 && head_dim != 128)) return DMR_ERR_UNSUPPORTED;
     return type == DMR_KV_BF16 || type == DMR_KV_E4M3 ? DMR_OK : DMR_ERR_UNSUPPORTED;
 }
@@ -36,7 +37,7 @@ dmr_status_t check_cache(const dmr_kv_cache_t *c, int32_t q_heads, dmr::CacheVie
     const dmr_status_t layout = check_layout(c->page_tokens, c->kv_heads, c->head_dim, c->type);
     if (layout != DMR_OK) return layout;
     if (c->pages <= 0 || c->pages > INT32_MAX / c->page_tokens) return DMR_ERR_SHAPE;
-    if (q_heads <= 0 || q_heads > 65536 || q_heads % c->kv_heads != 0) return DMR_ERR_SHAPE;
+    if (q_heads <= 0 || q_heads > kMaxHeads || q_heads % c->kv_heads != 0) return DMR_ERR_SHAPE;
     auto good = [](float s) { return s > 0.f && std::isfinite(s) && std::isfinite(1.0f / s); };
     if (!good(c->k_scale) || !good(c->v_scale)) return DMR_ERR_UNSUPPORTED;
     if (c->type == DMR_KV_BF16 && (c->k_scale != 1.0f || c->v_scale != 1.0f)) return DMR_ERR_UNSUPPORTED;
@@ -102,10 +103,10 @@ dmr_status_t dmr_kv_append(const dmr_kv_cache_t *cache, const uint16_t *d_qkv, i
 
 size_t dmr_attn_paged_workspace_bytes(int64_t rows, int64_t requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                                       int64_t max_query) {
-    if (rows <= 0 || rows > kMaxRows || requests <= 0 || requests > kMaxRequests || q_heads <= 0 || kv_heads <= 0 || q_heads > 65536 ||
+    if (rows <= 0 || rows > kMaxRows || requests <= 0 || requests > kMaxRequests || q_heads <= 0 || kv_heads <= 0 || q_heads > kMaxHeads ||
         q_heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_query <= 0)
         return 0;
-    return workspace_bytes(dmr::plan_attn(rows, requests, q_heads, kv_heads, max_query), kv_heads, head_dim);
+    return workspace_bytes(dmr::plan_attn(rows, requests, q_heads, kv_heads, max_query, INT64_MAX, false), kv_heads, head_dim);
 }
 
 dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, int64_t rows, int32_t q_heads, int64_t requests,
@@ -122,7 +123,8 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
     if (rows == 0 || requests == 0 || max_query == 0) return DMR_OK;
     if (!all_there(cache->d_k, cache->d_v, d_q, d_query_start, d_kv_lens, d_block_table, d_out)) return DMR_ERR_NULL;
     if (!all_aligned(cache->d_k, cache->d_v, d_q, d_out, d_ws) || !words_aligned(d_query_start, d_kv_lens, d_block_table)) return DMR_ERR_ALIGN;
-    const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, cache->kv_heads, max_query);
+    const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, cache->kv_heads, max_query, table_width * cache->page_tokens,
+                                               view.e4m3);
     const size_t need = workspace_bytes(plan, cache->kv_heads, cache->head_dim);
     if (need > 0 && (!d_ws || ws_bytes < need)) return DMR_ERR_WORKSPACE;
     if (plan.items * cache->kv_heads > INT32_MAX) return DMR_ERR_SHAPE;

@@ -55,15 +55,21 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_row
 
 }  // namespace
 
-AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query) {
+AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query, int64_t capacity, bool e4m3) {
     const int64_t G = q_heads / kv_heads, most = std::min(max_query, rows) * G;
     AttnPlan p;
     p.few = most <= 32;
     if (p.few) {
         p.tile_rows = most <= 16 ? 16 : 32;
-        const int64_t wanted = env_int("DMR_ATTN_FEW", 1024) / kv_heads;
-        p.split = requests * kv_heads < 8192;
-        p.parts = p.split ? (int)std::max<int64_t>(1, std::max(wanted, requests)) : 0;
+        // Parts: about what the chip holds at once of these workgroups, two (e4m3) to four (bf16, whose waves hold less) a CU.  Between
+        // half and twice that a decode step of the 7B-class decoder varies by 10 %.  us with 512 / 1024 in all: 1 x 32768 keys 27.8 /
+        // 29.4 (e4m3 19.1 / 22.7), 16 x 300..9000 62.2 / 58.6 (38.9 / 36.7), 32 x 1003 27.5 / 28.3 (18.6 / 21.6).  A large ragged
+        // batch gets finer parts, so that the last ones to start end soon: 96 x 1..8100 287 us with 96 to a head, 268 with 256.
+        const int64_t wanted = (e4m3 ? 512 : 1024) / kv_heads;
+        // no split, and no second launch, where the table is short (one request of 256 keys 4.8 us against 7.3; of 1003 13.1 against
+        // 8.1, as one CU reads 40 bytes a ns at most) or the requests fill the chip many times over
+        p.split = requests * kv_heads < 8192 && capacity > 256;
+        p.parts = p.split ? (int)std::max<int64_t>(1, std::max(wanted, 2 * requests)) : 0;
         p.items = requests + p.parts;
         return p;
     }

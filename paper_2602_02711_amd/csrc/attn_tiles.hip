@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kRows = 128;      // of a tile
 constexpr int kUnit = 64;       // keys staged at a time
-constexpr float kSlack = 8.f;   // the reference of the exponents may lag the largest score by 2^8
+constexpr float kMost = 4096.f; // a lane's 32 weights of a unit may sum to this before the reference of its row's exponents is moved
 
 typedef __attribute__((ext_vector_type(2))) __bf16 pair_bf16;
 
@@ -52,7 +52,9 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     f32x16 o[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
-    float m = kNoKey, l = 0.f;
+    // scores come out of the first product less the row's reference, the negative of which it starts from
+    f32x16 lag = f32x16{};
+    float l = 0.f;
     const int last_block = (rq.keys - 1) >> 4;
     const int key_row = 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), key_block = col >> 4;
 
@@ -106,18 +108,33 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     };
 
     // EDGE: some key of the unit is not seen by some row of the wave, or lies behind the request's last
-    auto unit = [&](int first, int buf, auto edge) {
+    auto unit = [&](int first, int buf, bool start, auto edge) {
         constexpr bool EDGE = decltype(edge)::value;
         const uint8_t *sk = lds + buf * (2 * STAGE) + key_block * BLOCK + h * 256 + key_row * 16;
         const uint8_t *sv = lds + buf * (2 * STAGE) + STAGE + h * (D * 16) + col * 16;
+        Frag k[2][D / 16], v[2][D / 16];
+        auto read_values = [&](int half) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                Frag w[D / 32];
+                read_frags<D / 32, 512>(sv + (2 * half + st) * BLOCK, sv + (2 * half + st) * BLOCK, w);
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) v[half][st * (D / 32) + t] = w[t];
+            }
+        };
         f32x16 s[2];
+        read_frags<D / 16, 512>(sk, sk, k[0]);
+        read_frags<D / 16, 512>(sk + 2 * BLOCK, sk + 2 * BLOCK, k[1]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            Frag k[D / 16];
-            read_frags<D / 16, 512>(sk + 2 * half * BLOCK, sk + 2 * half * BLOCK, k);
-            s[half] = f32x16{};
 #pragma unroll
-            for (int st = 0; st < D / 16; ++st) s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[st].v, q[st].v, s[half], 0, 0, 0);
+            for (int st = 0; st < D / 16; ++st)
+                s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[half][st].v, q[st].v, st ? s[half] : lag, 0, 0, 0);
+            if (half == 0) {
+                read_values(0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         // register i of half is key first + 32 half + 16 (i / 8) + 8 h + i % 8
         if constexpr (EDGE) {
@@ -127,46 +144,58 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[half][i] = 32 * half + 16 * (i >> 3) + (i & 7) < left ? s[half][i] : -INFINITY;
         }
-        float top = kNoKey;
+        Frag p[2][2];
+        float sum;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+            sum = 0.f;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(s[half][i], s[half][i + 1]));
-        top *= a.scale_log2;
-        // only then is the reference moved, and with it what was summed so far
-        if (__any(top > m + kSlack)) {
-            const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32))), fade = exp2_fast(m - to);
-            m = to;
-            l *= fade;
+                for (int i = 0; i < 16; i += 2) {
+                    const uint32_t w = pack_bf16x2(exp2_fast(s[half][i] * a.scale_log2), exp2_fast(s[half][i + 1] * a.scale_log2));
+                    p[half][i >> 3].w[(i & 7) >> 1] = w;
+                    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_bf16, w), __builtin_bit_cast(pair_bf16, 0x3F803F80u), sum, false);
+                }
+            if (pass || !(start || __any(!(sum <= kMost)))) break;
+            float top = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) o[t] *= fade;
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[half][i]);
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (top == -INFINITY || !(start || top > 0.f)) top = 0.f;
+            lag -= top;
+            s[0] -= top;
+            s[1] -= top;
+            if (!start) {
+                const float fade = exp2_fast(-top * a.scale_log2);
+                l *= fade;
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) o[t] *= fade;
+            }
         }
+        l += sum;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            Frag p[2];
+            if (half == 0) read_values(1);
+            if constexpr (EDGE) {      // values of slots behind the last key may hold anything, and 0 x NaN is NaN
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float e0 = exp2_fast(fmaf(s[half][i], a.scale_log2, -m)), e1 = exp2_fast(fmaf(s[half][i + 1], a.scale_log2, -m));
-                const uint32_t w = pack_bf16x2(e0, e1);
-                p[i >> 3].w[(i & 7) >> 1] = w;
-                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_bf16, w), __builtin_bit_cast(pair_bf16, 0x3F803F80u), l, false);
-            }
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                Frag v[D / 32];
-                read_frags<D / 32, 512>(sv + (2 * half + st) * BLOCK, sv + (2 * half + st) * BLOCK, v);
-                if constexpr (EDGE) {      // values of slots behind the last key may hold anything, and 0 x NaN is NaN
+                for (int st = 0; st < 2; ++st) {
                     const int left = rq.keys - (first + 32 * half + 16 * st + 8 * h);
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const uint32_t keep = (2 * w < left ? 0xFFFFu : 0u) | (2 * w + 1 < left ? 0xFFFF0000u : 0u);
 #pragma unroll
-                        for (int t = 0; t < D / 32; ++t) v[t].w[w] &= keep;
+                        for (int t = 0; t < D / 32; ++t) v[half][st * (D / 32) + t].w[w] &= keep;
                     }
                 }
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[t].v, p[st].v, o[t], 0, 0, 0);
             }
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t)
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[half][st * (D / 32) + t].v, p[half][st].v, o[t], 0, 0, 0);
         }
     };
 
@@ -177,8 +206,8 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     for (int u = u0; u < u1; ++u) {
         const int buf = (u - u0) & 1, first = u * kUnit;
         if (u + 1 < u1) request(u + 1, buf ^ 1);
-        if (first + kUnit <= wave_least) unit(first, buf, std::false_type{});
-        else if (first < wave_most) unit(first, buf, std::true_type{});
+        if (first + kUnit <= wave_least) unit(first, buf, u == u0, std::false_type{});
+        else if (first < wave_most) unit(first, buf, u == u0, std::true_type{});
         if (u + 1 < u1) arrive(buf ^ 1);
     }
     l += __shfl_xor(l, 32);
@@ -195,7 +224,7 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
         return;
     }
     const int64_t slot = ((int64_t)item * a.kv_heads + head) * kRows + 32 * wave + col;
-    if (h == 0) a.ml[slot] = make_float2(m, l);
+    if (h == 0) a.ml[slot] = make_float2(l > 0.f ? -lag[0] * a.scale_log2 : kNoKey, l);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll

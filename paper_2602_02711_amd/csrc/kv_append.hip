@@ -19,7 +19,7 @@ struct AppendArgs {
     uint16_t *q;
     uint8_t *k, *v;
     int64_t cache_slots;
-    int32_t q_heads, kv_heads, page_shift, heads_per_group;
+    int32_t q_heads, kv_heads, page_shift;
     float eps, inv_k_scale, inv_v_scale;
 };
 
@@ -38,25 +38,13 @@ __device__ __forceinline__ float other_half(float v) {
     return dpp_move<0x141>(dpp_move<0x1B>(v));               // lane j ^ 3, then 7 - j: j ^ 4
 }
 
-__device__ __forceinline__ float e4m3_range(float x) { return __builtin_amdgcn_fmed3f(x, -448.f, 448.f); }
-
-template <int D, bool E4M3, bool ADJACENT>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-    constexpr int LANES = D / 8, SLOTS = 256 / LANES;
-    const int lane = (int)threadIdx.x % LANES, head0 = (int)threadIdx.x / LANES;
-    const int64_t t = blockIdx.x;
-    const int heads = a.q_heads + 2 * a.kv_heads, rotated = a.q_heads + a.kv_heads;
-    const int64_t slot = a.slots[t];
-    const bool kept = slot >= 0 && slot < a.cache_slots;
-    const int per_page = a.page_shift - 4, in_page = (int)slot & ((1 << a.page_shift) - 1);
-    const int64_t page = slot >> a.page_shift;
-    const int block = in_page >> 4, tok = in_page & 15;
-    const int first = (int)blockIdx.y * a.heads_per_group, last = min(first + a.heads_per_group, heads);
-
-    // cosine and sine of this lane's pairs: 8 elements of one half, or 4 adjacent pairs
-    constexpr int PAIRS = ADJACENT ? 4 : 8;
+// Cosine and sine of the pairs that a lane holds: its 8 elements of one half, or 4 adjacent pairs.
+template <int D, bool ADJACENT>
+struct Turn {
+    static constexpr int PAIRS = ADJACENT ? 4 : 8;
     float cs[PAIRS], sn[PAIRS];
-    if (a.inv_freq && first < rotated) {
+    __device__ __forceinline__ void at(const AppendArgs &a, int64_t t, int lane) {
+        if (!a.inv_freq) return;
         const double pos = (double)a.positions[t];
 #pragma unroll
         for (int e = 0; e < PAIRS; ++e) {
@@ -66,86 +54,203 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             cs[e] = __builtin_amdgcn_cosf(f);
             sn[e] = __builtin_amdgcn_sinf(f);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < PAIRS; ++e) cs[e] = 1.f, sn[e] = 0.f;
     }
-    for (int base = first; base < last; base += SLOTS) {
-        const int h = base + head0;
-        const bool live = h < last;
-        // lanes of a head leave together; others' DPP moves stay within their own head
-        if (!live) continue;
-        const uint4 raw = reinterpret_cast<const uint4 *>(a.qkv)[(t * heads + h) * LANES + lane];
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        float x[8];
+};
+
+// A lane's 8 elements of query or key head h, normed and turned.
+template <int D, bool ADJACENT>
+__device__ __forceinline__ void norm_and_turn(const AppendArgs &a, const uint4 &raw, int h, int lane, const Turn<D, ADJACENT> &turn, float (&x)[8]) {
+    constexpr int LANES = D / 8;
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        x[2 * p] = __uint_as_float(w[p] << 16);
+        x[2 * p + 1] = __uint_as_float(w[p] & 0xFFFF0000u);
+    }
+    const uint16_t *gamma = h < a.q_heads ? a.gamma_q : a.gamma_k;
+    if (gamma) {
+        const float scale = rms_scale(head_sum<LANES>(sumsq_piece(raw)), 1.0f / D, a.eps);
+        const uint4 g = reinterpret_cast<const uint4 *>(gamma)[lane];
+        const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            x[2 * p] = __uint_as_float(w[p] << 16);
-            x[2 * p + 1] = __uint_as_float(w[p] & 0xFFFF0000u);
+            x[2 * p] = (x[2 * p] * scale) * __uint_as_float(gw[p] << 16);
+            x[2 * p + 1] = (x[2 * p + 1] * scale) * __uint_as_float(gw[p] & 0xFFFF0000u);
         }
-        if (h < rotated) {
-            const uint16_t *gamma = h < a.q_heads ? a.gamma_q : a.gamma_k;
-            if (gamma) {
-                const float scale = rms_scale(head_sum<LANES>(sumsq_piece(raw)), 1.0f / D, a.eps);
-                const uint4 g = reinterpret_cast<const uint4 *>(gamma)[lane];
-                const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
+    }
+    if (!a.inv_freq) return;
+    if constexpr (ADJACENT) {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    x[2 * p] = (x[2 * p] * scale) * __uint_as_float(gw[p] << 16);
-                    x[2 * p + 1] = (x[2 * p + 1] * scale) * __uint_as_float(gw[p] & 0xFFFF0000u);
-                }
-            }
-            if (a.inv_freq) {
-                if constexpr (ADJACENT) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float u = x[2 * e], v = x[2 * e + 1];
-                        x[2 * e] = u * cs[e] - v * sn[e];
-                        x[2 * e + 1] = v * cs[e] + u * sn[e];
-                    }
-                } else {
-                    const bool upper = lane >= LANES / 2;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float o = other_half<LANES>(x[e]);
-                        x[e] = x[e] * cs[e] + (upper ? o : -o) * sn[e];
-                    }
-                }
-            }
+        for (int e = 0; e < 4; ++e) {
+            const float u = x[2 * e], v = x[2 * e + 1];
+            x[2 * e] = u * turn.cs[e] - v * turn.sn[e];
+            x[2 * e + 1] = v * turn.cs[e] + u * turn.sn[e];
         }
-        if (h < a.q_heads) {
-            reinterpret_cast<uint4 *>(a.q)[(t * a.q_heads + h) * LANES + lane] =
-                make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-            continue;
-        }
-        if (!kept) continue;
-        const bool key = h < rotated;
-        const int kvh = h - (key ? a.q_heads : rotated);
-        const int64_t at = ((page * a.kv_heads + kvh) << per_page) + block;
-        if constexpr (E4M3) {
-            const float inv = key ? a.inv_k_scale : a.inv_v_scale;
-            uint32_t c[2];
+    } else {
+        const bool upper = lane >= LANES / 2;
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                int r = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[4 * p] * inv), e4m3_range(x[4 * p + 1] * inv), 0, false);
-                c[p] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[4 * p + 2] * inv), e4m3_range(x[4 * p + 3] * inv), r, true);
-            }
-            if (key) {
-                *reinterpret_cast<uint2 *>(a.k + at * (16 * D) + (lane >> 1) * 256 + tok * 16 + (lane & 1) * 8) = make_uint2(c[0], c[1]);
+        for (int e = 0; e < 8; ++e) {
+            const float o = other_half<LANES>(x[e]);
+            x[e] = x[e] * turn.cs[e] + (upper ? o : -o) * turn.sn[e];
+        }
+    }
+}
+
+__device__ __forceinline__ uint4 as_bf16(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+// Four values to e4m3, to nearest even, past the range to the largest.
+__device__ __forceinline__ uint32_t as_e4m3(float a, float b, float c, float d, float inv) {
+    auto range = [&](float v) { return __builtin_amdgcn_fmed3f(v * inv, -448.f, 448.f); };
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(range(a), range(b), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(range(c), range(d), lo, true);
+}
+__device__ __forceinline__ float bf16_at(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
+// Where the cache has slot `slot` of head kvh: block of 16 tokens, token in the block.
+struct Place {
+    int64_t block;
+    int tok;
+};
+__device__ __forceinline__ Place place_of(const AppendArgs &a, int64_t slot, int kvh) {
+    const int per_page = a.page_shift - 4, in_page = (int)slot & ((1 << a.page_shift) - 1);
+    return Place{((((slot >> a.page_shift) * a.kv_heads + kvh) << per_page) + (in_page >> 4)), in_page & 15};
+}
+
+// A lane's 8 elements of a key to their piece.
+template <int D, bool E4M3>
+__device__ __forceinline__ void store_key(const AppendArgs &a, const Place &at, int lane, const float (&x)[8]) {
+    if constexpr (E4M3)
+        *reinterpret_cast<uint2 *>(a.k + at.block * (16 * D) + (lane >> 1) * 256 + at.tok * 16 + (lane & 1) * 8) =
+            make_uint2(as_e4m3(x[0], x[1], x[2], x[3], a.inv_k_scale), as_e4m3(x[4], x[5], x[6], x[7], a.inv_k_scale));
+    else
+        *reinterpret_cast<uint4 *>(a.k + at.block * (32 * D) + lane * 256 + at.tok * 16) = as_bf16(x);
+}
+
+// Element d of a value to its place in the piece of its 8 or 16 tokens.
+template <int D, bool E4M3>
+__device__ __forceinline__ void store_value(const AppendArgs &a, const Place &at, int d, uint16_t v) {
+    if constexpr (E4M3)
+        a.v[at.block * (16 * D) + d * 16 + at.tok] = (uint8_t)as_e4m3(bf16_at(v), 0.f, 0.f, 0.f, a.inv_v_scale);
+    else
+        reinterpret_cast<uint16_t *>(a.v)[at.block * (16 * D) + (at.tok >> 3) * (D * 8) + d * 8 + (at.tok & 7)] = v;
+}
+
+constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.3 / 8.1 us (e4m3 7.9 / 9.7), 768 12.9 / 10.7 (11.7 / 11.7)
+
+// Few rows: a workgroup has 256 / (D / 8) heads of one row.
+template <int D, bool E4M3, bool ADJACENT>
+__global__ __launch_bounds__(256) void append_rows_kernel(AppendArgs a) {
+    constexpr int LANES = D / 8, SLOTS = 256 / LANES;
+    const int lane = (int)threadIdx.x % LANES, h = (int)blockIdx.y * SLOTS + (int)threadIdx.x / LANES;
+    const int64_t t = blockIdx.x;
+    const int heads = a.q_heads + 2 * a.kv_heads, rotated = a.q_heads + a.kv_heads;
+    if (h >= heads) return;      // lanes of a head leave together
+    const uint4 raw = reinterpret_cast<const uint4 *>(a.qkv)[(t * heads + h) * LANES + lane];
+    const int64_t slot = a.slots[t];
+    const bool kept = slot >= 0 && slot < a.cache_slots;
+    if (h >= rotated) {
+        if (!kept) return;
+        const Place at = place_of(a, slot, h - rotated);
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) store_value<D, E4M3>(a, at, 8 * lane + e, (uint16_t)(w[e >> 1] >> (16 * (e & 1))));
+        return;
+    }
+    Turn<D, ADJACENT> turn;
+    turn.at(a, t, lane);
+    float x[8];
+    norm_and_turn<D, ADJACENT>(a, raw, h, lane, turn, x);
+    if (h < a.q_heads) reinterpret_cast<uint4 *>(a.q)[(t * a.q_heads + h) * LANES + lane] = as_bf16(x);
+    else if (kept) store_key<D, E4M3>(a, place_of(a, slot, h - a.q_heads), lane, x);
+}
+
+// Many rows.  A workgroup has TOKENS rows of up to 8 query or key heads, whose angles it forms once and whose loads are all in flight
+// together; or 64 rows of one value head, which it turns in LDS: tokens that fill a piece of the cache leave as one store
+// of 16 bytes, the others, at the ends of a run of slots, element by element.  (With a thread's 8 elements of one token stored
+// one by one a wave's store fell into 64 lines: 8192 rows 77 us.)  Neighbouring rows go to one XCD, whose L2 then has the whole
+// lines that they share.
+constexpr int kHeadsAtOnce = 8, kValueRows = 64;
+template <int D, bool E4M3, bool ADJACENT>
+__global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int rows, int tiles, int chunks) {
+    constexpr int LANES = D / 8, TOKENS = 256 / LANES, RUN = E4M3 ? 16 : 8;
+    __shared__ __align__(16) uint16_t tile_of[kValueRows][D + 8];
+    __shared__ int slot_of[kValueRows];
+    __shared__ uint8_t lead[kValueRows], alone[kValueRows];
+    const int tid = (int)threadIdx.x, heads = a.q_heads + 2 * a.kv_heads, rotated = a.q_heads + a.kv_heads;
+    // block -> (tile of kValueRows rows, work of the tile): the tiles of an XCD are neighbours
+    const int works = chunks * (kValueRows / TOKENS) + a.kv_heads, per_xcd = (tiles + 7) / 8;
+    const int tile = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8) / works, work = (int)(blockIdx.x / 8) % works;
+    if (tile >= tiles) return;
+    if (work >= a.kv_heads) {
+        const int lane = tid % LANES, sub = (work - a.kv_heads) / chunks, first = (work - a.kv_heads) % chunks * kHeadsAtOnce;
+        const int64_t t = (int64_t)tile * kValueRows + sub * TOKENS + tid / LANES;
+        if (t >= rows) return;
+        const int n = min(kHeadsAtOnce, rotated - first);
+        u32x4_t raw[kHeadsAtOnce];
+        const u32x4_t *src = reinterpret_cast<const u32x4_t *>(a.qkv) + (t * heads + first) * LANES + lane;
+#pragma unroll
+        for (int i = 0; i < kHeadsAtOnce; ++i) raw[i] = src[min(i, n - 1) * LANES];
+        const int64_t slot = a.slots[t];
+        const bool kept = slot >= 0 && slot < a.cache_slots;
+        Turn<D, ADJACENT> turn;
+        turn.at(a, t, lane);
+#pragma unroll
+        for (int i = 0; i < kHeadsAtOnce; ++i) {
+            if (i >= n) break;
+            const int h = first + i;
+            float x[8];
+            norm_and_turn<D, ADJACENT>(a, make_uint4(raw[i][0], raw[i][1], raw[i][2], raw[i][3]), h, lane, turn, x);
+            if (h < a.q_heads) reinterpret_cast<uint4 *>(a.q)[(t * a.q_heads + h) * LANES + lane] = as_bf16(x);
+            else if (kept) store_key<D, E4M3>(a, place_of(a, slot, h - a.q_heads), lane, x);
+        }
+        return;
+    }
+    const int kvh = work;
+    const int64_t t0 = (int64_t)tile * kValueRows;
+    const int here = (int)min((int64_t)kValueRows, rows - t0);
+#pragma unroll
+    for (int i = 0; i < kValueRows / TOKENS; ++i) {
+        const int r = i * TOKENS + tid / LANES, lane = tid % LANES;
+        const uint4 v = reinterpret_cast<const uint4 *>(a.qkv)[((t0 + min(r, here - 1)) * heads + rotated + kvh) * LANES + lane];
+        *reinterpret_cast<uint4 *>(&tile_of[r][8 * lane]) = v;
+    }
+    if (tid < kValueRows) {
+        const int64_t slot = tid < here ? a.slots[t0 + tid] : -1;
+        slot_of[tid] = slot >= 0 && slot < a.cache_slots ? (int)slot : -1;
+    }
+    __syncthreads();
+    if (tid < kValueRows) {      // whether this row begins a whole piece
+        bool whole = tid + RUN <= kValueRows && slot_of[tid] >= 0 && slot_of[tid] % RUN == 0;
+        for (int i = 1; i < RUN; ++i) whole = whole && slot_of[min(tid + i, kValueRows - 1)] == slot_of[tid] + i;
+        lead[tid] = whole;
+    }
+    __syncthreads();
+    if (tid < kValueRows) {
+        bool in_piece = false;
+        for (int i = 0; i < RUN; ++i) in_piece = in_piece || (tid >= i && lead[tid - i]);
+        alone[tid] = slot_of[tid] >= 0 && !in_piece;
+    }
+    __syncthreads();
+    for (int r = tid / D; r < here; r += 256 / D) {
+        const int d = tid % D;
+        if (lead[r]) {
+            const Place at = place_of(a, slot_of[r], kvh);
+            if constexpr (E4M3) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = as_e4m3(bf16_at(tile_of[r + 4 * i][d]), bf16_at(tile_of[r + 4 * i + 1][d]), bf16_at(tile_of[r + 4 * i + 2][d]),
+                                   bf16_at(tile_of[r + 4 * i + 3][d]), a.inv_v_scale);
+                *reinterpret_cast<uint4 *>(a.v + at.block * (16 * D) + d * 16) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
-                uint8_t *dst = a.v + at * (16 * D) + lane * 128 + tok;
+                uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e * 16] = (uint8_t)(c[e >> 2] >> (8 * (e & 3)));
+                for (int i = 0; i < 4; ++i) w[i] = (uint32_t)tile_of[r + 2 * i][d] | ((uint32_t)tile_of[r + 2 * i + 1][d] << 16);
+                *reinterpret_cast<uint4 *>(a.v + at.block * (32 * D) + (at.tok >> 3) * (D * 16) + d * 16) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-        } else {
-            if (key) {
-                *reinterpret_cast<uint4 *>(a.k + at * (32 * D) + lane * 256 + tok * 16) =
-                    make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-            } else {
-                uint16_t *dst = reinterpret_cast<uint16_t *>(a.v + at * (32 * D)) + (tok >> 3) * (D * 8) + lane * 64 + (tok & 7);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e * 8] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));    // values go as they came
-            }
+        } else if (alone[r]) {
+            store_value<D, E4M3>(a, place_of(a, slot_of[r], kvh), d, tile_of[r][d]);
         }
     }
 }
@@ -155,20 +260,26 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
 hipError_t launch_kv_append(const CacheView &c, const uint16_t *qkv, int64_t rows, int q_heads, const uint16_t *gamma_q,
                             const uint16_t *gamma_k, float eps, const float *inv_freq, bool adjacent, const int32_t *positions,
                             const int32_t *slots, uint16_t *q, hipStream_t stream) {
-    AppendArgs a{qkv, gamma_q, gamma_k, inv_freq, positions, slots, q, c.k, c.v, c.pages << c.page_shift,
-                 q_heads, c.kv_heads, c.page_shift, 0, eps, 1.0f / c.k_scale, 1.0f / c.v_scale};
-    const int heads = q_heads + 2 * c.kv_heads, slots_per_group = 256 * 8 / c.D;
-    // few rows: a workgroup for every 16 (32) heads; many: one for all of a row's heads, which share its angles
-    a.heads_per_group = rows >= 512 ? heads : slots_per_group;
-    const dim3 grid((unsigned)rows, (unsigned)((heads + a.heads_per_group - 1) / a.heads_per_group));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
-    auto with = [&](auto d, auto e) {
+    const AppendArgs a{qkv, gamma_q, gamma_k, inv_freq, positions, slots, q, c.k, c.v, c.pages << c.page_shift,
+                       q_heads, c.kv_heads, c.page_shift, eps, 1.0f / c.k_scale, 1.0f / c.v_scale};
+    const int heads = q_heads + 2 * c.kv_heads, tokens = 256 * 8 / c.D;
+    auto with = [&](auto d, auto e, auto adj) {
         constexpr int D = decltype(d)::value;
-        constexpr bool E = decltype(e)::value;
-        if (adjacent) go(append_kernel<D, E, true>); else go(append_kernel<D, E, false>);
+        constexpr bool E = decltype(e)::value, A = decltype(adj)::value;
+        if (rows < env_int("DMR_APPEND_TILES", kTilesFrom)) {
+            const dim3 grid((unsigned)rows, (unsigned)((heads + tokens - 1) / tokens));
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_rows_kernel<D, E, A>), grid, dim3(256), 0, stream, a);
+        } else {
+            const int tiles = (int)((rows + kValueRows - 1) / kValueRows), chunks = (q_heads + c.kv_heads + kHeadsAtOnce - 1) / kHeadsAtOnce;
+            const int64_t blocks = (int64_t)8 * ((tiles + 7) / 8) * (chunks * (kValueRows / tokens) + c.kv_heads);
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_tiles_kernel<D, E, A>), dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rows, tiles, chunks);
+        }
+    };
+    auto pairs = [&](auto d, auto e) {
+        if (adjacent) with(d, e, std::true_type{}); else with(d, e, std::false_type{});
     };
     auto type = [&](auto d) {
-        if (c.e4m3) with(d, std::true_type{}); else with(d, std::false_type{});
+        if (c.e4m3) pairs(d, std::true_type{}); else pairs(d, std::false_type{});
     };
     if (c.D == 64) type(std::integral_constant<int, 64>{}); else type(std::integral_constant<int, 128>{});
     return hipGetLastError();
