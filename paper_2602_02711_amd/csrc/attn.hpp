@@ -143,11 +143,10 @@ __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int 
 
 // Eight e4m3 bytes to eight bf16 (exact).
 __device__ __forceinline__ uint4 bf16_of_e4m3(uint32_t lo, uint32_t hi) {
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
-    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
-    // a bf16 is the high half of its fp32: no rounding to do
-    auto pair = [](f32x2 p) { return __builtin_amdgcn_perm(__float_as_uint(p[1]), __float_as_uint(p[0]), 0x07060302u); };
-    return make_uint4(pair(a), pair(b), pair(c), pair(d));
+    auto pair = [](uint32_t w, auto upper) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, decltype(upper)::value));
+    };
+    return make_uint4(pair(lo, std::false_type{}), pair(lo, std::true_type{}), pair(hi, std::false_type{}), pair(hi, std::true_type{}));
 }
 
 // 2^x, x <= 0 or -inf.

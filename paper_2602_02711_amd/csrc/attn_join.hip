@@ -76,7 +76,7 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     p.tile_rows = 128;
     // tiles that so many rows of so many requests can make
     const int64_t tiles = std::min(requests * ((most + p.tile_rows - 1) / p.tile_rows), rows * G / p.tile_rows + requests);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(32, 512 / std::max<int64_t>(1, tiles * kv_heads)));
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(32, env_int("DMR_ATTN_PARTS", 512) / std::max<int64_t>(1, tiles * kv_heads)));
     p.items = tiles * p.parts;
     p.split = p.parts > 1;
     return p;
