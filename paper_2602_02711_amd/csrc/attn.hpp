@@ -178,7 +178,8 @@ struct AttnPlan {
     bool split;               // several items may belong to one tile: partial results, joined by a second kernel
 };
 constexpr int few_unit(bool e4m3) { return e4m3 ? 64 : 32; }      // keys that a wave of attn_few takes at a time
-AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query, int64_t capacity, bool e4m3);
+// `capacity`: tokens that a row of the block table can name; INT64_MAX gives a plan with no fewer items than any capacity's.
+AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int D, bool e4m3, int64_t max_query, int64_t capacity);
 inline size_t attn_part_floats(const AttnPlan &p, int kv_heads, int D) { return (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows * (size_t)D; }
 hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream);
 hipError_t launch_attn_few(const AttnArgs &a, const AttnPlan &p, int D, bool e4m3, hipStream_t stream);

@@ -106,7 +106,7 @@ size_t dmr_attn_paged_workspace_bytes(int64_t rows, int64_t requests, int32_t q_
     if (rows <= 0 || rows > kMaxRows || requests <= 0 || requests > kMaxRequests || q_heads <= 0 || kv_heads <= 0 || q_heads > kMaxHeads ||
         q_heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_query <= 0)
         return 0;
-    return workspace_bytes(dmr::plan_attn(rows, requests, q_heads, kv_heads, max_query, INT64_MAX, false), kv_heads, head_dim);
+    return workspace_bytes(dmr::plan_attn(rows, requests, q_heads, kv_heads, head_dim, false, max_query, INT64_MAX), kv_heads, head_dim);
 }
 
 dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, int64_t rows, int32_t q_heads, int64_t requests,
@@ -123,8 +123,8 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
     if (rows == 0 || requests == 0 || max_query == 0) return DMR_OK;
     if (!all_there(cache->d_k, cache->d_v, d_q, d_query_start, d_kv_lens, d_block_table, d_out)) return DMR_ERR_NULL;
     if (!all_aligned(cache->d_k, cache->d_v, d_q, d_out, d_ws) || !words_aligned(d_query_start, d_kv_lens, d_block_table)) return DMR_ERR_ALIGN;
-    const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, cache->kv_heads, max_query, table_width * cache->page_tokens,
-                                               view.e4m3);
+    const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, cache->kv_heads, view.D, view.e4m3, max_query,
+                                               table_width * cache->page_tokens);
     const size_t need = workspace_bytes(plan, cache->kv_heads, cache->head_dim);
     if (need > 0 && (!d_ws || ws_bytes < need)) return DMR_ERR_WORKSPACE;
     if (plan.items * cache->kv_heads > INT32_MAX) return DMR_ERR_SHAPE;

@@ -6,37 +6,60 @@ namespace dmr {
 
 namespace {
 
-// out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j over a tile's parts, M the largest m_j, in the order of the parts.  A workgroup has
-// a row: each wave takes every fourth part, a lane D / 64 elements.  UNIT: that of the attn_few kernel that split, 0: attn_tiles.
+// out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j over a tile's parts, M the largest m_j, in the order of the parts.
+//
+// UNIT > 0, after attn_few, whose tiles are few rows of many parts: a workgroup has a row, each wave every fourth part, a lane D / 64
+// elements.  UNIT = 0, after attn_tiles, the other way round: a wave has a row, and up to 32 parts.  (A workgroup for each row took
+// 35 us for the two parts of 1024 rows of 32 heads, a wave 10.)
 template <int D, int UNIT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_rows) {
     constexpr int E = D / 64;
-    __shared__ float sums[4][D + 1];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, in_tile = (int)blockIdx.y;
+    typedef float __attribute__((ext_vector_type(E))) elements;
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const int head = (int)blockIdx.x % a.kv_heads, at = (int)blockIdx.x / a.kv_heads;
     Share sh;
+    int in_tile;
     if constexpr (UNIT > 0) {
         sh = share_of_item<UNIT, true>(a, at, lane);
+        in_tile = (int)blockIdx.y;
     } else {
         sh = share_of_tile(a, at, tile_rows, lane);
         sh.first_item = at * a.parts;
+        in_tile = (int)blockIdx.y * 4 + wave;
     }
     const int row = sh.tile * tile_rows + in_tile;
     if (sh.b < 0 || row >= sh.rq.n * a.G || sh.parts <= 1) return;      // one part: its workgroup has stored the result
     const int64_t slot0 = ((int64_t)sh.first_item * a.kv_heads + head) * tile_rows + in_tile, step = (int64_t)a.kv_heads * tile_rows;
+    const int64_t out = ((int64_t)(sh.rq.first + row / a.G) * a.q_heads + head * a.G + row % a.G) * D;
+    auto wave_max = [](float v) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+        return v;
+    };
+    elements acc = {};
+    if constexpr (UNIT == 0) {
+        const float2 ml = lane < sh.parts ? a.ml[slot0 + lane * step] : make_float2(kNoKey, 0.f);
+        const float w = exp2_fast(ml.x - wave_max(ml.x)), L = wave64_sum(w * ml.y);
+        const elements *o = reinterpret_cast<const elements *>(a.part + slot0 * D) + lane;
+#pragma unroll 4
+        for (int j = 0; j < sh.parts; ++j)
+            acc += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), j)) * o[j * step * 64];
+        acc *= L > 0.f ? a.v_scale / L : 0.f;
+        if constexpr (E == 2) reinterpret_cast<uint32_t *>(a.out + out)[lane] = pack_bf16x2(acc[0], acc[1]);
+        else a.out[out + lane] = f32_to_bf16(acc[0]);
+        return;
+    }
+    __shared__ float sums[4][D + 1];
     float M = kNoKey;
     for (int j = lane; j < sh.parts; j += 64) M = fmaxf(M, a.ml[slot0 + j * step].x);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    float L = 0.f, acc[E] = {};
+    M = wave_max(M);
+    float L = 0.f;
 #pragma unroll 4
     for (int j = wave; j < sh.parts; j += 4) {
         const float2 ml = a.ml[slot0 + j * step];
-        const float *o = a.part + (slot0 + j * step) * D + lane * E;
         const float w = exp2_fast(ml.x - M);
         L = fmaf(w, ml.y, L);
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(w, o[e], acc[e]);
+        acc += w * reinterpret_cast<const elements *>(a.part + (slot0 + j * step) * D)[lane];
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = acc[e];
@@ -49,13 +72,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_row
     float o[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) o[e] = ((sums[0][2 * d + e] + sums[1][2 * d + e]) + (sums[2][2 * d + e] + sums[3][2 * d + e])) * r;
-    const int64_t out = ((int64_t)(sh.rq.first + row / a.G) * a.q_heads + head * a.G + row % a.G) * D;
     reinterpret_cast<uint32_t *>(a.out + out)[d] = pack_bf16x2(o[0], o[1]);
 }
 
 }  // namespace
 
-AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int64_t max_query, int64_t capacity, bool e4m3) {
+AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int D, bool e4m3, int64_t max_query, int64_t capacity) {
     const int64_t G = q_heads / kv_heads, most = std::min(max_query, rows) * G;
     AttnPlan p;
     p.few = most <= 32;
@@ -76,7 +98,20 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     p.tile_rows = 128;
     // tiles that so many rows of so many requests can make
     const int64_t tiles = std::min(requests * ((most + p.tile_rows - 1) / p.tile_rows), rows * G / p.tile_rows + requests);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(32, env_int("DMR_ATTN_PARTS", 512) / std::max<int64_t>(1, tiles * kv_heads)));
+    // Parts: the least estimated time, in ns, among those that two workgroups a CU can serve at once.  A workgroup alone on its CU takes
+    // 17 ns for a key of its tile, two take 29 (D = 64: 0.6 of that); joining costs a launch and the partial results' way to memory and
+    // back.  us with 1 part / as many as 256 / 512 workgroups: 64 rows over 2000 keys 39 / 19 / 26, 300 over 8000 137 / 63 / 61, 512
+    // over 32768 543 / 311 / 272, 1024 over 1024 25 / 25 / 35, over 16000 288 / 293 / 258, 8 x 12 over 4000 72 / 31 / 43.
+    const int64_t wgs = std::max<int64_t>(1, tiles * kv_heads), most_parts = std::max<int64_t>(1, std::min<int64_t>(32, 2 * kCus / wgs));
+    auto estimate = [&](int64_t parts) {
+        const double key = (D == 64 ? 0.6 : 1.0) * (wgs * parts <= kCus ? 17.0 : 29.0);
+        return (double)capacity / (double)parts * key +
+               (parts > 1 ? 4000.0 + (double)parts * (double)rows * q_heads * D * 8.0 / 4000.0 : 0.0);
+    };
+    p.parts = (int)most_parts;
+    if (capacity < INT64_MAX)
+        for (int64_t n = most_parts - 1; n > 0; --n)
+            if (estimate(n) <= estimate(p.parts)) p.parts = (int)n;
     p.items = tiles * p.parts;
     p.split = p.parts > 1;
     return p;
@@ -84,7 +119,7 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
 
 hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, bool e4m3, hipStream_t stream) {
     const int64_t tiles = p.few ? a.requests : a.items / p.parts;
-    const dim3 grid((unsigned)(tiles * a.kv_heads), (unsigned)std::min(rows, p.tile_rows));
+    const dim3 grid((unsigned)(tiles * a.kv_heads), (unsigned)(p.few ? std::min(rows, p.tile_rows) : (std::min(rows, p.tile_rows) + 3) / 4));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tile_rows); };
     auto split_by = [&](auto unit) {
         constexpr int U = decltype(unit)::value;
