@@ -26,6 +26,7 @@ struct AttnArgs {
     float scale_log2;         // softmax scale * key scale * log2(e)
     float v_scale;
     int32_t items;            // per kv head, of the grid
+    int32_t max_tiles;        // of a request
     int32_t parts;            // attn_tiles: parts of every tile's keys;  attn_few: as share_of_item says, 0: one item per request
 };
 
@@ -81,12 +82,13 @@ struct Share {
     Request rq;
 };
 
-// Item -> tile where every tile has a.parts parts: request b has ceil(n G / tile_rows) tiles.
+// Item -> tile where every tile has a.parts parts: request b has ceil(n G / tile_rows) tiles, and no more than max_query asks for, so
+// that one with more rows takes no other's.
 __device__ __forceinline__ Share share_of_tile(const AttnArgs &a, int tile, int tile_rows, int lane) {
     for (int base = 0; base < a.requests; base += 64) {
         const int i = base + lane;
         const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
-        const uint32_t tiles = (uint32_t)((r.n * a.G + tile_rows - 1) / tile_rows), upto = wave_scan(tiles);
+        const uint32_t tiles = (uint32_t)min((int)(((int64_t)r.n * a.G + tile_rows - 1) / tile_rows), a.max_tiles), upto = wave_scan(tiles);
         const uint64_t above = __ballot((int)upto > tile);
         if (above) {
             const int l = __builtin_ctzll(above);
@@ -174,7 +176,7 @@ struct AttnPlan {
     bool few;                 // attn_few: one tile of 16 or 32 rows per request
     int tile_rows;            // (token, query head) rows of a tile
     int64_t items;            // workgroups per kv head
-    int parts;                // AttnArgs::parts
+    int parts, max_tiles;     // AttnArgs
     bool split;               // several items may belong to one tile: partial results, joined by a second kernel
 };
 constexpr int few_unit(bool e4m3) { return e4m3 ? 64 : 32; }      // keys that a wave of attn_few takes at a time

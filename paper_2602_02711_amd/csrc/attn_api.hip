@@ -7,6 +7,7 @@ namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxRequests = int64_t(1) << 20;
 constexpr int32_t kMaxHeads = 4096;
+constexpr int64_t kMaxGroups = UINT32_MAX / 256;      // workgroups of 256 threads in a launch
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 template <typename... P>
@@ -127,14 +128,14 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
                                                table_width * cache->page_tokens);
     const size_t need = workspace_bytes(plan, cache->kv_heads, cache->head_dim);
     if (need > 0 && (!d_ws || ws_bytes < need)) return DMR_ERR_WORKSPACE;
-    if (plan.items * cache->kv_heads > INT32_MAX) return DMR_ERR_SHAPE;
+    if (plan.items * cache->kv_heads > kMaxGroups) return DMR_ERR_SHAPE;
     const size_t part = align256(dmr::attn_part_floats(plan, cache->kv_heads, cache->head_dim) * 4);
     const dmr::AttnArgs a{d_q, d_out, view.k, view.v, d_query_start, d_kv_lens, d_block_table,
                           plan.split ? static_cast<float *>(d_ws) : nullptr,
                           plan.split ? reinterpret_cast<float2 *>(static_cast<uint8_t *>(d_ws) + part) : nullptr,
                           (int32_t)rows, (int32_t)requests, (int32_t)table_width, q_heads, cache->kv_heads, q_heads / cache->kv_heads,
                           (int32_t)cache->pages, view.page_shift, scale_log2, view.v_scale,
-                          (int32_t)plan.items, plan.parts};
+                          (int32_t)plan.items, plan.max_tiles, plan.parts};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = plan.few ? dmr::launch_attn_few(a, plan, view.D, view.e4m3, s) : dmr::launch_attn_tiles(a, view.D, view.e4m3, s);
     if (e != hipSuccess || !plan.split) return hip_status(e);

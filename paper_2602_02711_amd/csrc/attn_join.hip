@@ -81,6 +81,7 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     const int64_t G = q_heads / kv_heads, most = std::min(max_query, rows) * G;
     AttnPlan p;
     p.few = most <= 32;
+    p.max_tiles = 1;
     if (p.few) {
         p.tile_rows = most <= 16 ? 16 : 32;
         // Parts: about what the chip holds at once of these workgroups, two (e4m3) to four (bf16, whose waves hold less) a CU.  Between
@@ -97,7 +98,8 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     }
     p.tile_rows = 128;
     // tiles that so many rows of so many requests can make
-    const int64_t tiles = std::min(requests * ((most + p.tile_rows - 1) / p.tile_rows), rows * G / p.tile_rows + requests);
+    p.max_tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
+    const int64_t tiles = std::min(requests * p.max_tiles, rows * G / p.tile_rows + requests);
     // Parts: the least estimated time, in ns, among those that two workgroups a CU can serve at once.  A workgroup alone on its CU takes
     // 17 ns for a key of its tile, two take 29 (D = 64: 0.6 of that); joining costs a launch and the partial results' way to memory and
     // back.  us with 1 part / as many as 256 / 512 workgroups: 64 rows over 2000 keys 39 / 19 / 26, 300 over 8000 137 / 63 / 61, 512

@@ -40,8 +40,9 @@ def build(seed, news, lens, heads, kv_heads, dim, page, cache, sharp=2.0, extra_
         table[b, :held[b]] = order[at:at + held[b]]
         at += held[b]
         l = max(l, 0)
-        kb = (torch.randn(l, kv_heads, dim, generator=gen) / ks).to(dt)
-        vb = ((torch.randn(l, kv_heads, dim, generator=gen) + 0.3) / vs).to(dt)
+        # (a value past the range of e4m3, once in 10^7, would be cast to NaN)
+        kb = (torch.randn(l, kv_heads, dim, generator=gen) / ks).clamp(-448, 448).to(dt)
+        vb = ((torch.randn(l, kv_heads, dim, generator=gen) + 0.3) / vs).clamp(-448, 448).to(dt)
         t = torch.arange(l)
         slot = torch.from_numpy(table[b])[t // page] * page + t % page
         k[slot], v[slot] = kb.float(), vb.float()
@@ -140,6 +141,28 @@ def test_many_requests(requests, cache):
     check(requests, [1] * requests, rng.integers(0, 400, requests).tolist(), 4, 1, 64, 16, cache)
     news = rng.integers(0, 40, requests).tolist()
     check(requests, news, [n + int(o) for n, o in zip(news, rng.integers(0, 90, requests))], 4, 2, 64, 16, cache)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_batches_that_are_not_split(cache):
+    """Requests of even lengths that fill the chip, and a batch too large to be worth a split."""
+    rng = np.random.default_rng(40)
+    check(40, [1] * 40, rng.integers(290, 310, 40).tolist(), 8, 8, 64, 32, cache)
+    lens = rng.integers(0, 60, 1100).tolist()
+    lens[700] = 2000
+    check(41, [1] * 1100, lens, 8, 8, 64, 64, cache)
+
+
+@pytest.mark.parametrize("news,most,heads", [([300, 90, 40], 90, 8), ([9, 3, 1], 3, 4), ([50, 8, 2], 8, 4)])
+def test_a_request_of_more_rows_than_max_query_takes_nothing_from_others(news, most, heads):
+    lens = [n + 200 for n in news]
+    pool, q, keys, table = build(23, news, lens, heads, heads // 4, 64, 32, "bf16")
+    start = np.concatenate([[0], np.cumsum(news)])
+    out = torch.full((sum(news), heads * 64), SENTINEL, dtype=torch.bfloat16, device=DEV)
+    dmr.dmr_attn_paged(pool, q.to(DEV), heads, dev(start), dev(lens), dev(table), most, 0.125, out=out)
+    want, tol = expect(q, keys, news, heads, 64, 0.125, rounding_of_weights(most, heads, heads // 4))
+    ok = ((out.cpu().double().view(-1, heads, 64) - want).abs() <= tol).flatten(1).all(1)
+    assert ok[:most].all() and ok[news[0]:].all()
 
 
 @pytest.mark.parametrize("sharp", [0.0, 0.01, 30.0])
