@@ -8,14 +8,15 @@
 // as the pieces of the value pool do.
 //
 // The keys and values of the next 64 arrive while these are worked on: bf16 ones by loads into the other half of the buffer, e4m3
-// ones through registers, where a thread makes them bf16 once for all four waves.  One barrier for each 64 keys; a second workgroup on
-// the CU works through it.
+// ones through registers, where a thread makes them bf16 once for all four waves, before the last products (at the unit's end 4 %
+// slower).  One barrier for each 64 keys; a second workgroup on the CU works through it.
 //
-// Bound by power: 2048 rows over 32768 keys run at 2.0 GHz.  995 us, 1.07 PFLOP/s, where a bf16 product of 8192^3 reaches 1.21.  What
+// Bound by power: 2048 rows over 32768 keys run at 2.0 GHz, 955 us, 1.12 PFLOP/s, where a bf16 product of 8192^3 reaches 1.21.  What
 // brought it there, from 1840 us: loads ahead and masks at the edges alone, 1072; a loop of its own for units without an edge (the
-// branch inside kept copies of all accumulators) and the maximum looked for only when a sum says so, 1000; every operand read
-// from LDS eight MFMAs before its own, 940 on other data.  Eight waves on the same keys, 64 rows to a wave, units of 32 and 128 keys
-// and weights among the other half's products were level or slower.
+// branch inside kept copies of all accumulators) and the maximum looked for only when a sum says so, 9 % less; every operand read
+// from LDS eight MFMAs before its own, 6 %; the tiles with the most keys first, 8 .. 12 % of a causal prompt; priority for the wave
+// that is at its products, 2 %.  Eight waves on the same keys, 64 rows to a wave, 32 keys at a time, and the weights of one half
+// among the other's products were level or slower.
 #include "attn.hpp"
 #include "lds_loads.hpp"
 
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
             }
         }
     };
-    auto arrive = [&](int buf) {
+    // e4m3 pieces that have come, as bf16 into LDS (after the last unit nothing has, and nothing reads what this leaves)
+    auto deposit = [&](int buf) {
         if constexpr (E4M3) {
             uint8_t *dst = lds + buf * (2 * STAGE);
 #pragma unroll
@@ -118,10 +120,11 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
                 *reinterpret_cast<uint4 *>(dv) = bf16_of_e4m3(hv[i][0], hv[i][1]);
                 *reinterpret_cast<uint4 *>(dv + D * 16) = bf16_of_e4m3(hv[i][2], hv[i][3]);
             }
-            wait_lds();
-        } else {
-            wait_loads<0>();
         }
+    };
+    // what was requested or deposited lies in LDS, and every wave is done with the buffer before
+    auto settle = [&] {
+        if constexpr (E4M3) wait_lds(); else wait_loads<0>();
         bare_barrier();
     };
 
@@ -177,6 +180,7 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
             }
         };
 
+        __builtin_amdgcn_s_setprio(1);
         read_frags<KS, 512>(sk, sk, k[0]);
         __builtin_amdgcn_sched_barrier(0);
         read_frags<KS, 512>(sk + 2 * BLOCK, sk + 2 * BLOCK, k[1]);
@@ -192,6 +196,7 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[half][i] = 32 * half + 16 * (i >> 3) + (i & 7) < left ? s[half][i] : -INFINITY;
         }
+        __builtin_amdgcn_s_setprio(0);
         float sum = weigh();
         // the first unit comes here (its reference is still kNoKey), and then few: what was summed so far fades to the new reference
         if (__builtin_expect(__any(!(sum <= kMost)), 0)) {
@@ -209,15 +214,18 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
             sum = weigh();
         }
         l += sum;
+        __builtin_amdgcn_s_setprio(1);
         read_values(1);
         outputs(0);
         read_among_products<2 * VT, 2>();
+        deposit(buf ^ 1);
         outputs(1);
     };
 
     if (u0 < u1) {
         request(u0, 0);
-        arrive(0);
+        deposit(0);
+        settle();
     }
     const int whole = min(u1, max(u0, wave_least / kUnit));
     int u = u0;
@@ -225,13 +233,14 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
         const int buf = (u - u0) & 1;
         if (u + 1 < u1) request(u + 1, buf ^ 1);
         unit(u * kUnit, buf, std::false_type{});
-        if (u + 1 < u1) arrive(buf ^ 1);
+        if (u + 1 < u1) settle();
     }
     for (; u < u1; ++u) {
         const int buf = (u - u0) & 1;
         if (u + 1 < u1) request(u + 1, buf ^ 1);
         if (u * kUnit < wave_most) unit(u * kUnit, buf, std::true_type{});
-        if (u + 1 < u1) arrive(buf ^ 1);
+        else deposit(buf ^ 1);
+        if (u + 1 < u1) settle();
     }
     l += __shfl_xor(l, 32);
     if (row0 + 32 * wave + col >= rows) return;
