@@ -136,7 +136,7 @@ __device__ __forceinline__ void store_value(const AppendArgs &a, const Place &at
         reinterpret_cast<uint16_t *>(a.v)[at.block * (16 * D) + (at.tok >> 3) * (D * 8) + d * 8 + (at.tok & 7)] = v;
 }
 
-constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.3 / 8.1 us (e4m3 7.9 / 9.7), 768 12.9 / 10.7 (11.7 / 11.7)
+constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.2 / 8.6 us (e4m3 7.8 / 10.4), 768 12.9 / 9.3 (11.9 / 10.8)
 
 // Few rows: a workgroup has 256 / (D / 8) heads of one row.
 template <int D, bool E4M3, bool ADJACENT>
@@ -165,23 +165,21 @@ __global__ __launch_bounds__(256) void append_rows_kernel(AppendArgs a) {
     else if (kept) store_key<D, E4M3>(a, place_of(a, slot, h - a.q_heads), lane, x);
 }
 
-// Many rows.  A workgroup has TOKENS rows of up to 8 query or key heads, whose angles it forms once and whose loads are all in flight
+// Many rows.  A workgroup has TOKENS rows of up to 4 query or key heads, whose angles it forms once and whose loads are all in flight
 // together; or 64 rows of one value head, which it turns in LDS: tokens that fill a piece of the cache leave as one store
 // of 16 bytes, the others, at the ends of a run of slots, element by element.  (With a thread's 8 elements of one token stored
-// one by one a wave's store fell into 64 lines: 8192 rows 77 us.)  Neighbouring rows go to one XCD, whose L2 then has the whole
-// lines that they share.
-constexpr int kHeadsAtOnce = 8, kValueRows = 64;
+// one by one a wave's store fell into 64 lines: 8192 rows 77 us.)  The projection is read, and queries are written, past the caches:
+// 53 -> 42 us for 8192 rows of the 7B-class decoder, 4.8 TB/s, where a copy of as many bytes takes 39.
+constexpr int kHeadsAtOnce = 4, kValueRows = 64;
 template <int D, bool E4M3, bool ADJACENT>
-__global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int rows, int tiles, int chunks) {
+__global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int rows, int chunks) {
     constexpr int LANES = D / 8, TOKENS = 256 / LANES, RUN = E4M3 ? 16 : 8;
     __shared__ __align__(16) uint16_t tile_of[kValueRows][D + 8];
     __shared__ int slot_of[kValueRows];
     __shared__ uint8_t lead[kValueRows], alone[kValueRows];
     const int tid = (int)threadIdx.x, heads = a.q_heads + 2 * a.kv_heads, rotated = a.q_heads + a.kv_heads;
-    // block -> (tile of kValueRows rows, work of the tile): the tiles of an XCD are neighbours
-    const int works = chunks * (kValueRows / TOKENS) + a.kv_heads, per_xcd = (tiles + 7) / 8;
-    const int tile = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8) / works, work = (int)(blockIdx.x / 8) % works;
-    if (tile >= tiles) return;
+    const int works = chunks * (kValueRows / TOKENS) + a.kv_heads;      // of a tile of kValueRows rows
+    const int tile = (int)blockIdx.x / works, work = (int)blockIdx.x % works;
     if (work >= a.kv_heads) {
         const int lane = tid % LANES, sub = (work - a.kv_heads) / chunks, first = (work - a.kv_heads) % chunks * kHeadsAtOnce;
         const int64_t t = (int64_t)tile * kValueRows + sub * TOKENS + tid / LANES;
@@ -190,7 +188,7 @@ __global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int row
         u32x4_t raw[kHeadsAtOnce];
         const u32x4_t *src = reinterpret_cast<const u32x4_t *>(a.qkv) + (t * heads + first) * LANES + lane;
 #pragma unroll
-        for (int i = 0; i < kHeadsAtOnce; ++i) raw[i] = src[min(i, n - 1) * LANES];
+        for (int i = 0; i < kHeadsAtOnce; ++i) raw[i] = __builtin_nontemporal_load(src + min(i, n - 1) * LANES);
         const int64_t slot = a.slots[t];
         const bool kept = slot >= 0 && slot < a.cache_slots;
         Turn<D, ADJACENT> turn;
@@ -201,8 +199,12 @@ __global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int row
             const int h = first + i;
             float x[8];
             norm_and_turn<D, ADJACENT>(a, make_uint4(raw[i][0], raw[i][1], raw[i][2], raw[i][3]), h, lane, turn, x);
-            if (h < a.q_heads) reinterpret_cast<uint4 *>(a.q)[(t * a.q_heads + h) * LANES + lane] = as_bf16(x);
-            else if (kept) store_key<D, E4M3>(a, place_of(a, slot, h - a.q_heads), lane, x);
+            if (h < a.q_heads) {
+                const uint4 w = as_bf16(x);
+                __builtin_nontemporal_store(u32x4_t{w.x, w.y, w.z, w.w}, reinterpret_cast<u32x4_t *>(a.q) + (t * a.q_heads + h) * LANES + lane);
+            } else if (kept) {
+                store_key<D, E4M3>(a, place_of(a, slot, h - a.q_heads), lane, x);
+            }
         }
         return;
     }
@@ -212,8 +214,8 @@ __global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int row
 #pragma unroll
     for (int i = 0; i < kValueRows / TOKENS; ++i) {
         const int r = i * TOKENS + tid / LANES, lane = tid % LANES;
-        const uint4 v = reinterpret_cast<const uint4 *>(a.qkv)[((t0 + min(r, here - 1)) * heads + rotated + kvh) * LANES + lane];
-        *reinterpret_cast<uint4 *>(&tile_of[r][8 * lane]) = v;
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.qkv) + ((t0 + min(r, here - 1)) * heads + rotated + kvh) * LANES + lane);
+        *reinterpret_cast<u32x4_t *>(&tile_of[r][8 * lane]) = v;
     }
     if (tid < kValueRows) {
         const int64_t slot = tid < here ? a.slots[t0 + tid] : -1;
@@ -271,8 +273,8 @@ hipError_t launch_kv_append(const CacheView &c, const uint16_t *qkv, int64_t row
             hipLaunchKernelGGL(HIP_KERNEL_NAME(append_rows_kernel<D, E, A>), grid, dim3(256), 0, stream, a);
         } else {
             const int tiles = (int)((rows + kValueRows - 1) / kValueRows), chunks = (q_heads + c.kv_heads + kHeadsAtOnce - 1) / kHeadsAtOnce;
-            const int64_t blocks = (int64_t)8 * ((tiles + 7) / 8) * (chunks * (kValueRows / tokens) + c.kv_heads);
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_tiles_kernel<D, E, A>), dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rows, tiles, chunks);
+            const int64_t blocks = (int64_t)tiles * (chunks * (kValueRows / tokens) + c.kv_heads);
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(append_tiles_kernel<D, E, A>), dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)rows, chunks);
         }
     };
     auto pairs = [&](auto d, auto e) {
