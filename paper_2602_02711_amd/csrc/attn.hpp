@@ -21,7 +21,8 @@ struct AttnArgs {
     const uint8_t *k, *v;
     const int32_t *start, *lens, *table;
     float *part;              // [item][kv head][tile rows][D] unnormalised outputs
-    float2 *ml;               // [item][kv head][tile rows]: largest score (log2 units), sum
+    float2 *ml;               // [item][kv head][tile rows]: reference of the exponents (log2 units), sum
+    int2 *split;              // attn_few: [request] first item, parts, for attn_join
     int32_t rows, requests, width, q_heads, kv_heads, G, pages, page_shift;
     float scale_log2;         // softmax scale * key scale * log2(e)
     float v_scale;
@@ -104,9 +105,9 @@ __device__ __forceinline__ Share share_of_tile(const AttnArgs &a, int tile, int 
 // C = max(kMinUnits, ceil(U / a.parts)), a request of u units has ceil(u / C) parts, one at least: no more than a.parts + requests
 // items, whatever the lengths.  A batch that gives every CU a workgroup and whose longest request is no longer than 3 / 2 of the mean
 // is not split.  Each workgroup forms the same sums from the lengths on the device, so that a captured call splits the lengths
-// of its replay and a ragged batch's longest request decides nothing.  `item` is an item's number, or with BY_REQUEST a request's.
+// of its replay and a ragged batch's longest request decides nothing.
 constexpr int kMinUnits = 4;      // a unit for each wave of a workgroup
-template <int UNIT, bool BY_REQUEST>
+template <int UNIT>
 __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int lane) {
     uint64_t total = 0;
     uint32_t longest = 0, some = 0;
@@ -128,14 +129,10 @@ __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int 
         const int i = base + lane;
         const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
         const uint32_t items = r.n > 0 ? std::max(1u, (units_of(r) + C - 1) / C) : 0u, upto = wave_scan(items);
-        int l = item - base;
-        if constexpr (!BY_REQUEST) {
-            const uint64_t above = __ballot(before + (int)upto > item);
-            l = above ? __builtin_ctzll(above) : 64;
-        }
-        if (l < 64) {
-            const int first = before + (int)lane_value(upto - items, l), parts = (int)lane_value(items, l);
-            return Share{base + l, 0, BY_REQUEST ? 0 : item - first, parts, first,
+        const uint64_t above = __ballot(before + (int)upto > item);
+        if (above) {
+            const int l = __builtin_ctzll(above), first = before + (int)lane_value(upto - items, l);
+            return Share{base + l, 0, item - first, (int)lane_value(items, l), first,
                          Request{(int)lane_value(r.first, l), (int)lane_value(r.n, l), (int)lane_value(r.keys, l)}};
         }
         before += (int)lane_value(upto, 63);
@@ -182,10 +179,9 @@ struct AttnPlan {
 constexpr int few_unit(bool e4m3) { return e4m3 ? 64 : 32; }      // keys that a wave of attn_few takes at a time
 // `capacity`: tokens that a row of the block table can name; INT64_MAX gives a plan with no fewer items than any capacity's.
 AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, int D, bool e4m3, int64_t max_query, int64_t capacity);
-inline size_t attn_part_floats(const AttnPlan &p, int kv_heads, int D) { return (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows * (size_t)D; }
 hipError_t launch_attn_tiles(const AttnArgs &a, int D, bool e4m3, hipStream_t stream);
 hipError_t launch_attn_few(const AttnArgs &a, const AttnPlan &p, int D, bool e4m3, hipStream_t stream);
 // Joins the parts that a split call left; `rows` of a tile at most.
-hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, bool e4m3, hipStream_t stream);
+hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, hipStream_t stream);
 
 }  // namespace dmr

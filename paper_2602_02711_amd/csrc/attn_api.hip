@@ -49,11 +49,18 @@ dmr_status_t check_cache(const dmr_kv_cache_t *c, int32_t q_heads, dmr::CacheVie
 
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Partial outputs, then their (maximum, sum).
-size_t workspace_bytes(const dmr::AttnPlan &p, int kv_heads, int D) {
-    if (!p.split) return 0;
-    const size_t part = dmr::attn_part_floats(p, kv_heads, D) * 4;
-    return align256(part) + part / (size_t)D * 2;
+// Partial outputs, their (reference, sum), and what a request's items are.
+struct Workspace {
+    size_t ml, split, bytes;
+};
+Workspace workspace_of(const dmr::AttnPlan &p, int64_t requests, int kv_heads, int D) {
+    if (!p.split) return Workspace{0, 0, 0};
+    const size_t rows = (size_t)p.items * (size_t)kv_heads * (size_t)p.tile_rows;
+    Workspace w;
+    w.ml = align256(rows * (size_t)D * sizeof(float));
+    w.split = w.ml + align256(rows * sizeof(float2));
+    w.bytes = w.split + (p.few ? (size_t)requests * sizeof(int2) : 0);
+    return w;
 }
 
 }  // namespace
@@ -107,7 +114,8 @@ size_t dmr_attn_paged_workspace_bytes(int64_t rows, int64_t requests, int32_t q_
     if (rows <= 0 || rows > kMaxRows || requests <= 0 || requests > kMaxRequests || q_heads <= 0 || kv_heads <= 0 || q_heads > kMaxHeads ||
         q_heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_query <= 0)
         return 0;
-    return workspace_bytes(dmr::plan_attn(rows, requests, q_heads, kv_heads, head_dim, false, max_query, INT64_MAX), kv_heads, head_dim);
+    const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, kv_heads, head_dim, false, max_query, INT64_MAX);
+    return workspace_of(plan, requests, kv_heads, head_dim).bytes;
 }
 
 dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, int64_t rows, int32_t q_heads, int64_t requests,
@@ -126,21 +134,20 @@ dmr_status_t dmr_attn_paged(const dmr_kv_cache_t *cache, const uint16_t *d_q, in
     if (!all_aligned(cache->d_k, cache->d_v, d_q, d_out, d_ws) || !words_aligned(d_query_start, d_kv_lens, d_block_table)) return DMR_ERR_ALIGN;
     const dmr::AttnPlan plan = dmr::plan_attn(rows, requests, q_heads, cache->kv_heads, view.D, view.e4m3, max_query,
                                                table_width * cache->page_tokens);
-    const size_t need = workspace_bytes(plan, cache->kv_heads, cache->head_dim);
-    if (need > 0 && (!d_ws || ws_bytes < need)) return DMR_ERR_WORKSPACE;
+    const Workspace need = workspace_of(plan, requests, cache->kv_heads, cache->head_dim);
+    if (need.bytes > 0 && (!d_ws || ws_bytes < need.bytes)) return DMR_ERR_WORKSPACE;
     if (plan.items * cache->kv_heads > kMaxGroups) return DMR_ERR_SHAPE;
-    const size_t part = align256(dmr::attn_part_floats(plan, cache->kv_heads, cache->head_dim) * 4);
+    uint8_t *ws = plan.split ? static_cast<uint8_t *>(d_ws) : nullptr;
     const dmr::AttnArgs a{d_q, d_out, view.k, view.v, d_query_start, d_kv_lens, d_block_table,
-                          plan.split ? static_cast<float *>(d_ws) : nullptr,
-                          plan.split ? reinterpret_cast<float2 *>(static_cast<uint8_t *>(d_ws) + part) : nullptr,
+                          reinterpret_cast<float *>(ws), reinterpret_cast<float2 *>(ws ? ws + need.ml : nullptr),
+                          reinterpret_cast<int2 *>(ws ? ws + need.split : nullptr),
                           (int32_t)rows, (int32_t)requests, (int32_t)table_width, q_heads, cache->kv_heads, q_heads / cache->kv_heads,
                           (int32_t)cache->pages, view.page_shift, scale_log2, view.v_scale,
                           (int32_t)plan.items, plan.max_tiles, plan.parts};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = plan.few ? dmr::launch_attn_few(a, plan, view.D, view.e4m3, s) : dmr::launch_attn_tiles(a, view.D, view.e4m3, s);
     if (e != hipSuccess || !plan.split) return hip_status(e);
-    return hip_status(dmr::launch_attn_join(a, plan, (int)std::min<int64_t>(std::min(max_query, rows) * a.G, plan.tile_rows), view.D,
-                                            view.e4m3, s));
+    return hip_status(dmr::launch_attn_join(a, plan, (int)std::min<int64_t>(std::min(max_query, rows) * a.G, plan.tile_rows), view.D, s));
 }
 
 }  // extern "C"

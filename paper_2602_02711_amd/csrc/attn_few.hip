@@ -38,7 +38,8 @@ __global__ __launch_bounds__(256, E4M3 && D == 128 && NQ == 2 ? 1 : 2) void attn
     if (a.parts == 0) {
         sh = Share{item, 0, 0, 1, item, request_at(a, item)};
     } else {
-        sh = share_of_item<UNIT, false>(a, item, lane);
+        sh = share_of_item<UNIT>(a, item, lane);
+        if (sh.b >= 0 && sh.part == 0 && head == 0 && tid == 0) a.split[sh.b] = make_int2(sh.first_item, sh.parts);
     }
     const Request rq = sh.rq;
     const int rows = min(rq.n * a.G, ROWS);

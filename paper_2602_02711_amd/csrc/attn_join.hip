@@ -8,10 +8,10 @@ namespace {
 
 // out = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j over a tile's parts, M the largest m_j, in the order of the parts.
 //
-// UNIT > 0, after attn_few, whose tiles are few rows of many parts: a workgroup has a row, each wave every fourth part, a lane D / 64
-// elements.  UNIT = 0, after attn_tiles, the other way round: a wave has a row, and up to 32 parts.  (A workgroup for each row took
+// FEW, after attn_few, whose tiles are few rows of many parts: a workgroup has a row, each wave every fourth part, a lane D / 64
+// elements.  Else, after attn_tiles, the other way round: a wave has a row, and up to 32 parts.  (A workgroup for each row took
 // 35 us for the two parts of 1024 rows of 32 heads, a wave 10.)
-template <int D, int UNIT>
+template <int D, bool FEW>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_rows) {
     constexpr int E = D / 64;
     typedef float __attribute__((ext_vector_type(E))) elements;
@@ -19,8 +19,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_row
     const int head = (int)blockIdx.x % a.kv_heads, at = (int)blockIdx.x / a.kv_heads;
     Share sh;
     int in_tile;
-    if constexpr (UNIT > 0) {
-        sh = share_of_item<UNIT, true>(a, at, lane);
+    if constexpr (FEW) {
+        const int2 split = a.split[at];      // not written for a request without rows
+        sh = Share{at, 0, 0, split.y, split.x, request_at(a, at)};
         in_tile = (int)blockIdx.y;
     } else {
         sh = share_of_tile(a, at, tile_rows, lane);
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_row
         return v;
     };
     elements acc = {};
-    if constexpr (UNIT == 0) {
+    if constexpr (!FEW) {
         const float2 ml = lane < sh.parts ? a.ml[slot0 + lane * step] : make_float2(kNoKey, 0.f);
         const float w = exp2_fast(ml.x - wave_max(ml.x)), L = wave64_sum(w * ml.y);
         const elements *o = reinterpret_cast<const elements *>(a.part + slot0 * D) + lane;
@@ -119,17 +120,15 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     return p;
 }
 
-hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, bool e4m3, hipStream_t stream) {
+hipError_t launch_attn_join(const AttnArgs &a, const AttnPlan &p, int rows, int D, hipStream_t stream) {
     const int64_t tiles = p.few ? a.requests : a.items / p.parts;
     const dim3 grid((unsigned)(tiles * a.kv_heads), (unsigned)(p.few ? std::min(rows, p.tile_rows) : (std::min(rows, p.tile_rows) + 3) / 4));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, p.tile_rows); };
-    auto split_by = [&](auto unit) {
-        constexpr int U = decltype(unit)::value;
-        if (D == 64) go(attn_join_kernel<64, U>); else go(attn_join_kernel<128, U>);
-    };
-    if (!p.few) split_by(std::integral_constant<int, 0>{});
-    else if (e4m3) split_by(std::integral_constant<int, few_unit(true)>{});
-    else split_by(std::integral_constant<int, few_unit(false)>{});
+    if (p.few) {
+        if (D == 64) go(attn_join_kernel<64, true>); else go(attn_join_kernel<128, true>);
+    } else {
+        if (D == 64) go(attn_join_kernel<64, false>); else go(attn_join_kernel<128, false>);
+    }
     return hipGetLastError();
 }
 
