@@ -483,28 +483,17 @@ def dmr_qlinear_bf16_forward_fused(w: torch.Tensor, pro: int, inp: torch.Tensor,
 # ---- paged attention -----------------------------------------------------------------------------
 
 _I32 = (torch.int32,)
-_U8 = (torch.uint8,)
 
 
-def _group(dev: int, dtypes, names, tensors):
-    """Addresses of contiguous tensors of one of ``dtypes`` on device ``dev``.  These calls take up to ten tensors and launch kernels of
-    3 us: checked together a tensor costs 0.17 us, one by one through _dev 0.4."""
-    found = []
-    for t in tensors:
-        try:
-            good = t.dtype in dtypes and t.get_device() == dev and t.is_contiguous()
-        except AttributeError:
-            good = False
-        if not good:
-            name = names[len(found)]
+def _refuse(dev: int, *tensors):
+    """Which of (name, tensor, dtypes) a call cannot take.  The calls below look at up to ten tensors and launch kernels of 3 us, so they
+    look in one expression, 0.15 us a tensor, and come here only if something is wrong."""
+    for name, t, dtypes in tensors:
+        if t is not None:
             _dev(t, name, dtypes)
-            raise ValueError(f"{name} must be on the current device")
-        found.append(t.data_ptr())
-    return found
-
-
-def _raw_stream(dev: int, stream) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+            if t.get_device() != dev:
+                raise ValueError(f"{name} must be on the current device")
+    raise ValueError("a tensor of this call cannot be used")
 
 
 class KvCache:
@@ -562,10 +551,24 @@ def dmr_kv_assign(new_tokens: torch.Tensor, lens: torch.Tensor, free_pages: torc
     start, kv_lens, positions, slots, left = out
     if start.numel() != n + 1 or kv_lens.numel() != n or positions.numel() != rows or slots.numel() != rows or left.numel() != 2:
         raise ValueError("out must be query_start [requests + 1], kv_lens [requests], positions [rows], slots [rows], left [2]")
-    at = _group(dev, _I32, ("new_tokens", "lens", "free_pages", "free_count", "block_table", "query_start", "kv_lens", "positions", "slots",
-                            "left"),
-                (new_tokens, lens, free_pages, free_count, block_table, start, kv_lens, positions, slots, left))
-    status = lib().dmr_kv_assign(n, rows, width, page_tokens, free_pages.numel(), *at, _raw_stream(dev, stream))
+    i32 = torch.int32
+    if not (new_tokens.dtype is i32 and new_tokens.is_contiguous() and new_tokens.get_device() == dev
+            and lens.dtype is i32 and lens.is_contiguous() and lens.get_device() == dev
+            and free_pages.dtype is i32 and free_pages.is_contiguous() and free_pages.get_device() == dev
+            and free_count.dtype is i32 and free_count.is_contiguous() and free_count.get_device() == dev
+            and block_table.dtype is i32 and block_table.is_contiguous() and block_table.get_device() == dev
+            and start.dtype is i32 and start.is_contiguous() and start.get_device() == dev
+            and kv_lens.dtype is i32 and kv_lens.is_contiguous() and kv_lens.get_device() == dev
+            and positions.dtype is i32 and positions.is_contiguous() and positions.get_device() == dev
+            and slots.dtype is i32 and slots.is_contiguous() and slots.get_device() == dev
+            and left.dtype is i32 and left.is_contiguous() and left.get_device() == dev):
+        _refuse(dev, ("new_tokens", new_tokens, _I32), ("lens", lens, _I32), ("free_pages", free_pages, _I32), ("free_count", free_count, _I32),
+                ("block_table", block_table, _I32), ("query_start", start, _I32), ("kv_lens", kv_lens, _I32), ("positions", positions, _I32),
+                ("slots", slots, _I32), ("left", left, _I32))
+    status = lib().dmr_kv_assign(n, rows, width, page_tokens, free_pages.numel(), new_tokens.data_ptr(), lens.data_ptr(),
+                                 free_pages.data_ptr(), free_count.data_ptr(), block_table.data_ptr(), start.data_ptr(), kv_lens.data_ptr(),
+                                 positions.data_ptr(), slots.data_ptr(), left.data_ptr(),
+                                 torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
     if status:
         raise DmrError(status, "dmr_kv_assign")
     return tuple(out)
@@ -589,26 +592,24 @@ def dmr_kv_append(cache: KvCache, qkv: torch.Tensor, q_heads: int, positions: to
         out = torch.empty((rows, q_heads * D), dtype=torch.bfloat16, device=qkv.device)
     elif out.shape != (rows, q_heads * D):
         raise ValueError("out must be [rows][q_heads head_dim]")
-    px, po = _group(dev, _BF16, ("qkv", "out"), (qkv, out))
-    pg = ph = pf = pp = None
-    if gamma_q is not None:
-        (pg,) = _group(dev, _BF16, ("gamma_q",), (gamma_q,))
-        if gamma_q.shape != (D,):
-            raise ValueError("gamma_q must be [head_dim]")
-    if gamma_k is not None:
-        (ph,) = _group(dev, _BF16, ("gamma_k",), (gamma_k,))
-        if gamma_k.shape != (D,):
-            raise ValueError("gamma_k must be [head_dim]")
-    if inv_freq is not None:
-        (pf,) = _group(dev, (torch.float32,), ("inv_freq",), (inv_freq,))
-        if inv_freq.shape != (D // 2,):
-            raise ValueError("inv_freq must be [head_dim / 2]")
-    if positions is None:
-        (ps,) = _group(dev, _I32, ("slots",), (slots,))
-    else:
-        ps, pp = _group(dev, _I32, ("slots", "positions"), (slots, positions))
-    status = lib().dmr_kv_append(cache._ref, px, rows, q_heads, pg, ph, eps, pf, DMR_ROPE_ADJACENT if interleaved else DMR_ROPE_HALVES, pp, ps,
-                                 po, _raw_stream(dev, stream))
+    f32, i32 = torch.float32, torch.int32
+    if not (qkv.dtype in _BF16 and qkv.is_contiguous() and qkv.get_device() == dev
+            and out.dtype in _BF16 and out.is_contiguous() and out.get_device() == dev
+            and slots.dtype is i32 and slots.is_contiguous() and slots.get_device() == dev
+            and (positions is None or (positions.dtype is i32 and positions.is_contiguous() and positions.get_device() == dev))
+            and (gamma_q is None or (gamma_q.dtype in _BF16 and gamma_q.is_contiguous() and gamma_q.get_device() == dev))
+            and (gamma_k is None or (gamma_k.dtype in _BF16 and gamma_k.is_contiguous() and gamma_k.get_device() == dev))
+            and (inv_freq is None or (inv_freq.dtype is f32 and inv_freq.is_contiguous() and inv_freq.get_device() == dev))):
+        _refuse(dev, ("qkv", qkv, _BF16), ("out", out, _BF16), ("slots", slots, _I32), ("positions", positions, _I32),
+                ("gamma_q", gamma_q, _BF16), ("gamma_k", gamma_k, _BF16), ("inv_freq", inv_freq, (f32,)))
+    if (gamma_q is not None and gamma_q.shape != (D,)) or (gamma_k is not None and gamma_k.shape != (D,)):
+        raise ValueError("gamma_q and gamma_k must be [head_dim]")
+    if inv_freq is not None and inv_freq.shape != (D // 2,):
+        raise ValueError("inv_freq must be [head_dim / 2]")
+    status = lib().dmr_kv_append(cache._ref, qkv.data_ptr(), rows, q_heads, None if gamma_q is None else gamma_q.data_ptr(),
+                                 None if gamma_k is None else gamma_k.data_ptr(), eps, None if inv_freq is None else inv_freq.data_ptr(),
+                                 DMR_ROPE_ADJACENT if interleaved else DMR_ROPE_HALVES, None if positions is None else positions.data_ptr(),
+                                 slots.data_ptr(), out.data_ptr(), torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
     if status:
         raise DmrError(status, "dmr_kv_append")
     return out
@@ -636,19 +637,23 @@ def dmr_attn_paged(cache: KvCache, q: torch.Tensor, q_heads: int, query_start: t
         out = torch.zeros((rows, width), dtype=torch.bfloat16, device=q.device)
     elif out.shape != (rows, width):
         raise ValueError("out must be [rows][q_heads head_dim]")
-    pq, po = _group(dev, _BF16, ("q", "out"), (q, out))
-    ps, pl, pt = _group(dev, _I32, ("query_start", "kv_lens", "block_table"), (query_start, kv_lens, block_table))
-    pw, ws_bytes = None, 0
+    i32 = torch.int32
+    if not (q.dtype in _BF16 and q.is_contiguous() and q.get_device() == dev
+            and out.dtype in _BF16 and out.is_contiguous() and out.get_device() == dev
+            and query_start.dtype is i32 and query_start.is_contiguous() and query_start.get_device() == dev
+            and kv_lens.dtype is i32 and kv_lens.is_contiguous() and kv_lens.get_device() == dev
+            and block_table.dtype is i32 and block_table.is_contiguous() and block_table.get_device() == dev
+            and (workspace is None or (workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == dev))):
+        _refuse(dev, ("q", q, _BF16), ("out", out, _BF16), ("query_start", query_start, _I32), ("kv_lens", kv_lens, _I32),
+                ("block_table", block_table, _I32), ("workspace", workspace, (torch.uint8,)))
     if workspace is None:
-        ws_bytes = dmr_attn_paged_workspace_bytes(rows, n, q_heads, cache.kv_heads, D, max_query)
-        if ws_bytes > 0:
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)    # device memory only
-            pw = workspace.data_ptr()
-    else:
-        (pw,) = _group(dev, _U8, ("workspace",), (workspace,))
-        ws_bytes = workspace.numel()
-    status = lib().dmr_attn_paged(cache._ref, pq, rows, q_heads, n, ps, pl, pt, columns, max_query, scale, po, pw, ws_bytes,
-                                  _raw_stream(dev, stream))
+        need = dmr_attn_paged_workspace_bytes(rows, n, q_heads, cache.kv_heads, D, max_query)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)    # device memory only
+    status = lib().dmr_attn_paged(cache._ref, q.data_ptr(), rows, q_heads, n, query_start.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr(),
+                                  columns, max_query, scale, out.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                                  0 if workspace is None else workspace.numel(),
+                                  torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
     if status:
         raise DmrError(status, "dmr_attn_paged")
     return out
