@@ -198,11 +198,45 @@ def mixed_step(args, dmr, synth, torch, dev):
     print(json.dumps(result), flush=True)
 
 
+def chain_attention(args, dmr, torch, dev, gen, layers, rows):
+    """The attention block of chain_step with --context N: every row is a request's new token, the last of N keys of its own (32 query
+    and 8 key heads of 128, pages of 64 tokens, bf16, a cache for each layer).  Returns attend(layer, qkv, out); layer 0 also
+    gives the step its pages, positions and slots."""
+    heads, kv_heads, dim, page, n = 32, 8, 128, 64, args.context
+    width = -(-n // page)
+    held = -(-(n - 1) // page)
+    order = torch.randperm(rows * width, generator=gen, device=dev).int()
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=dev)
+    table[:, :held] = order[:rows * held].view(rows, held)
+    ints = lambda m, v=0: torch.full((m,), v, dtype=torch.int32, device=dev)
+    new, lens, stack = ints(rows, 1), ints(rows, n - 1), torch.cat([order[rows * held:], ints(1)])
+    count = ints(1, rows * (width - held))
+    out = (ints(rows + 1), ints(rows), ints(rows), ints(rows), ints(2))
+    caches = [dmr.KvCache.empty(rows * width, page, kv_heads, dim, device=dev) for _ in range(layers)]
+    for c in caches:
+        for pool in (c.k, c.v):
+            pool.copy_(torch.randn(pool.shape, generator=gen, device=dev, dtype=torch.bfloat16))
+    gq, gk = (1.0 + 0.1 * torch.randn((2, dim), generator=gen, device=dev)).to(torch.bfloat16)
+    freq = (1e6 ** (-torch.arange(0, dim, 2, device=dev).double() / dim)).float()
+    attn = torch.empty((rows, heads * dim), dtype=torch.bfloat16, device=dev)
+    ws = torch.empty(max(16, dmr.dmr_attn_paged_workspace_bytes(rows, rows, heads, kv_heads, dim, 1)), dtype=torch.uint8, device=dev)
+
+    def attend(layer, qkv, q):
+        if layer == 0:
+            dmr.dmr_kv_assign(new, lens, stack, count, table, page, rows, out=out)
+        start, kv_lens, positions, slots, _ = out
+        dmr.dmr_kv_append(caches[layer], qkv, heads, positions, slots, gq, gk, 1e-6, freq, out=q)
+        return dmr.dmr_attn_paged(caches[layer], q, heads, start, kv_lens, table, 1, dim ** -0.5, out=attn, workspace=ws)
+
+    return attend
+
+
 def chain_step(args, dmr, synth, torch, dev):
     """One decode step (M = 1) of a 32-layer 7B-class decoder as a dependent chain of its Linear layers
     with the glue between them: per layer RMSNorm -> qkv, attn_out + residual, RMSNorm -> gate_up,
-    SwiGLU -> down + residual.  Attention itself is not a Linear and is not modelled: the first 4096
-    columns of the qkv output stand in for its result, so that the shapes chain.  Timed four ways: the
+    SwiGLU -> down + residual.  The first 4096 columns of the qkv output stand in for attention's result,
+    so that the shapes chain, unless --context asks for attention itself (three more launches a layer
+    and one a step, in all four variants).  Timed four ways: the
     glue fused into the Linear launches (4 launches per layer) or as kernels of its own (rmsnorm x 2,
     swiglu, residual add x 2: 9 launches per layer), for the INT4 copy and for the bf16 copy."""
     G, LAYERS, H, I, M = synth.GROUP, 32, 4096, 14336, args.m
@@ -231,6 +265,7 @@ def chain_step(args, dmr, synth, torch, dev):
             "norm": torch.empty((M, H), dtype=torch.bfloat16, device=dev),
             "h": [torch.empty((M, H), dtype=torch.bfloat16, device=dev) for _ in range(3)],
             "ws": torch.empty(64 << 20, dtype=torch.uint8, device=dev)}
+    attend = chain_attention(args, dmr, torch, dev, gen, LAYERS, M) if args.context else None
     torch.cuda.synchronize()
     log(f"[bench] 128 layers resident after {time.time() - t0:.1f}s")
     stream = torch.cuda.Stream()
@@ -274,7 +309,9 @@ def chain_step(args, dmr, synth, torch, dev):
                     out.add_(res)
 
             lin("qkv", R, h, g1, None, bufs["qkv"])
-            if M == 1:
+            if attend:
+                attn = attend(li, bufs["qkv"], bufs["q"])
+            elif M == 1:
                 attn = bufs["qkv"][:, :H]                 # attention stand-in: the q slice (a view at M = 1)
             else:
                 attn = bufs["q"]
@@ -324,7 +361,8 @@ def chain_step(args, dmr, synth, torch, dev):
         "ms_per_step": round(t, 5), "higher_is_better": False, "scaling": "weak", "vs_baseline": None,
         "dtype": "bf16", "data": "synthetic",
         "config": {"workload": f"32 layers x (rmsnorm->qkv, attn_out+residual, rmsnorm->gate_up, swiglu->down+residual), "
-                               f"M={M}, attention replaced by the q slice, hip-graph replay"},
+                               f"M={M}, " + (f"attention of each row over {args.context} keys in pages" if args.context else
+                                             "attention replaced by the q slice") + ", hip-graph replay"},
         "us_per_step": {"int4_fused": round(times[(True, True)] * 1e3, 1),
                         "int4_unfused": round(times[(True, False)] * 1e3, 1),
                         "bf16_fused": round(times[(False, True)] * 1e3, 1),
@@ -580,6 +618,8 @@ def main():
                     help="decode_sweep (default, the headline metric) or full_step: all 129 Linear layers of "
                          "a 32-layer 7B-class decoder per step")
     ap.add_argument("--m", type=int, default=1, help="rows of activations for --workload full_step / chain_step")
+    ap.add_argument("--context", type=int, default=0,
+                    help="keys of each row's request in --workload chain_step: attention over a paged cache (0: the q slice of qkv stands in)")
     ap.add_argument("--ms", default=MS_DEFAULT, help="row counts for --workload layer_sweep / w3_sweep (there the default is 1)")
     ap.add_argument("--shapes", default="", help="comma-separated shape names for --workload layer_sweep")
     args = ap.parse_args()
