@@ -60,19 +60,23 @@ __device__ __forceinline__ int64_t uniform_block_offset(const AttnArgs &a, const
     return (((((int64_t)page * a.kv_heads + head) << per_page) + (block & ((1 << per_page) - 1)))) * BLOCK_BYTES;
 }
 
-// Inclusive sum over the wave's lanes.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+// Inclusive scan over the wave's lanes under `op`, whose neutral element is 0.
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, Op op) {
     auto from = [](uint32_t u, auto ctrl, auto rows) {
         return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
     };
     typedef std::integral_constant<int, 0xF> all;
-    v += from(v, std::integral_constant<int, 0x111>{}, all{});      // row_shr 1, 2, 4, 8: within rows of 16
-    v += from(v, std::integral_constant<int, 0x112>{}, all{});
-    v += from(v, std::integral_constant<int, 0x114>{}, all{});
-    v += from(v, std::integral_constant<int, 0x118>{}, all{});
-    v += from(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});      // row_bcast 15: rows 1 and 3
-    v += from(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});      // row_bcast 31: rows 2 and 3
+    v = op(v, from(v, std::integral_constant<int, 0x111>{}, all{}));      // row_shr 1, 2, 4, 8: within rows of 16
+    v = op(v, from(v, std::integral_constant<int, 0x112>{}, all{}));
+    v = op(v, from(v, std::integral_constant<int, 0x114>{}, all{}));
+    v = op(v, from(v, std::integral_constant<int, 0x118>{}, all{}));
+    v = op(v, from(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{}));      // row_bcast 15: rows 1 and 3
+    v = op(v, from(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{}));      // row_bcast 31: rows 2 and 3
     return v;
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    return wave_scan(v, [](uint32_t a, uint32_t b) { return a + b; });
 }
 __device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 
@@ -112,22 +116,22 @@ __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int 
     uint64_t total = 0;
     uint32_t longest = 0, some = 0;
     auto units_of = [](const Request &r) { return (uint32_t)(r.n > 0 ? (r.keys + UNIT - 1) / UNIT : 0); };
+    auto request_of = [&](int i) { return i < a.requests ? request_at(a, i) : Request{0, 0, 0}; };
+    Request r;      // of this lane, in the round at hand: up to 64 requests are read once
     for (int base = 0; base < a.requests; base += 64) {
-        const int i = base + lane;
-        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
+        r = request_of(base + lane);
         const uint32_t u = units_of(r);
         total += lane_value(wave_scan(u), 63);
-        longest = std::max(longest, u);
+        longest = std::max(longest, lane_value(wave_scan(u, [](uint32_t x, uint32_t y) { return std::max(x, y); }), 63));
         some += (uint32_t)__popcll(__ballot(r.n > 0));
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) longest = std::max(longest, (uint32_t)__shfl_xor((int)longest, d));
-    uint32_t C = (uint32_t)std::max<uint64_t>(kMinUnits, (total + (uint32_t)a.parts - 1) / (uint32_t)a.parts);
+    const uint32_t parts = (uint32_t)a.parts;
+    const uint32_t even = total >> 31 ? (uint32_t)((total + parts - 1) / parts) : ((uint32_t)total + parts - 1) / parts;
+    uint32_t C = std::max((uint32_t)kMinUnits, even);
     if (some * (uint32_t)a.kv_heads >= (uint32_t)kCus && (uint64_t)longest * some * 2 <= total * 3) C = std::max(C, longest);
     int before = 0;
     for (int base = 0; base < a.requests; base += 64) {
-        const int i = base + lane;
-        const Request r = i < a.requests ? request_at(a, i) : Request{0, 0, 0};
+        if (a.requests > 64) r = request_of(base + lane);
         const uint32_t items = r.n > 0 ? std::max(1u, (units_of(r) + C - 1) / C) : 0u, upto = wave_scan(items);
         const uint64_t above = __ballot(before + (int)upto > item);
         if (above) {

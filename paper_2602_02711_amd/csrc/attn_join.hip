@@ -50,29 +50,52 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int tile_row
         else a.out[out + lane] = f32_to_bf16(acc[0]);
         return;
     }
-    __shared__ float sums[4][D + 1];
-    float M = kNoKey;
-    for (int j = lane; j < sh.parts; j += 64) M = fmaxf(M, a.ml[slot0 + j * step].x);
-    M = wave_max(M);
-    float L = 0.f;
-#pragma unroll 4
-    for (int j = wave; j < sh.parts; j += 4) {
-        const float2 ml = a.ml[slot0 + j * step];
-        const float w = exp2_fast(ml.x - M);
-        L = fmaf(w, ml.y, L);
-        acc += w * reinterpret_cast<const elements *>(a.part + (slot0 + j * step) * D)[lane];
+    __shared__ float sums[4][D];
+    __shared__ float2 mls[4];
+    // a wave's parts eight at a time, requested with their references, which they then fade to
+    constexpr int AHEAD = 8;
+    float m = kNoKey, L = 0.f;
+    for (int j0 = wave; j0 < sh.parts; j0 += 4 * AHEAD) {
+        float2 ml[AHEAD];
+        elements o[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t at_j = slot0 + min(j0 + 4 * i, sh.parts - 1) * step;
+            ml[i] = a.ml[at_j];
+            o[i] = reinterpret_cast<const elements *>(a.part + at_j * D)[lane];
+        }
+        float to = m;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) to = fmaxf(to, ml[i].x);
+        const float fade = exp2_fast(m - to);
+        m = to;
+        L *= fade;
+        acc *= fade;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float w = j0 + 4 * i < sh.parts ? exp2_fast(ml[i].x - m) : 0.f;
+            L = fmaf(w, ml[i].y, L);
+            acc += w * o[i];
+        }
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = acc[e];
-    if (lane == 0) sums[wave][D] = L;
+    if (lane == 0) mls[wave] = make_float2(m, L);
     __syncthreads();
     const int d = (int)threadIdx.x;
     if (d >= D / 2) return;
-    const float l = (sums[0][D] + sums[1][D]) + (sums[2][D] + sums[3][D]);
-    const float r = l > 0.f ? a.v_scale / l : 0.f;
-    float o[2];
+    const float M = fmaxf(fmaxf(mls[0].x, mls[1].x), fmaxf(mls[2].x, mls[3].x));
+    float l = 0.f, o[2] = {};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) o[e] = ((sums[0][2 * d + e] + sums[1][2 * d + e]) + (sums[2][2 * d + e] + sums[3][2 * d + e])) * r;
+    for (int w = 0; w < 4; ++w) {
+        const float f = exp2_fast(mls[w].x - M);
+        l = fmaf(f, mls[w].y, l);
+        o[0] = fmaf(f, sums[w][2 * d], o[0]);
+        o[1] = fmaf(f, sums[w][2 * d + 1], o[1]);
+    }
+    const float r = l > 0.f ? a.v_scale / l : 0.f;
+    o[0] *= r;
+    o[1] *= r;
     reinterpret_cast<uint32_t *>(a.out + out)[d] = pack_bf16x2(o[0], o[1]);
 }
 
