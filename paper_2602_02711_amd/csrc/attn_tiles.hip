@@ -11,12 +11,12 @@
 // ones through registers, where a thread makes them bf16 once for all four waves, before the last products (at the unit's end 4 %
 // slower).  One barrier for each 64 keys; a second workgroup on the CU works through it.
 //
-// Bound by power: 2048 rows over 32768 keys run at 2.0 GHz, 955 us, 1.12 PFLOP/s, where a bf16 product of 8192^3 reaches 1.21.  What
-// brought it there, from 1840 us: loads ahead and masks at the edges alone, 1072; a loop of its own for units without an edge (the
-// branch inside kept copies of all accumulators) and the maximum looked for only when a sum says so, 9 % less; every operand read
-// from LDS eight MFMAs before its own, 6 %; the tiles with the most keys first, 8 .. 12 % of a causal prompt; priority for the wave
-// that is at its products, 2 %.  Eight waves on the same keys, 64 rows to a wave, 32 keys at a time, and the weights of one half
-// among the other's products were level or slower.
+// Bound by power: 2048 rows over 32768 keys run at 1.7 GHz with the matrix pipes busy 64 % of the cycles, as long bf16 products do;
+// 920 .. 955 us, 1.12 .. 1.16 PFLOP/s, where one of 8192^3 reaches 1.21.  What brought it there, from 1840 us: loads ahead and masks at
+// the edges alone, 1072; a loop of its own for units without an edge (the branch inside kept copies of all accumulators) and the
+// maximum looked for only when a sum says so, 9 % less; every operand read from LDS eight MFMAs before its own, 6 %; the tiles with
+// the most keys first, 8 .. 12 % of a causal prompt; priority for the wave that is at its products, 2 %.  Eight waves on the same
+// keys, 64 rows to a wave, 32 keys at a time, and the weights of one half among the other's products were level or slower.
 #include "attn.hpp"
 #include "lds_loads.hpp"
 
