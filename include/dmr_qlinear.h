@@ -261,7 +261,7 @@ dmr_status_t dmr_kv_assign(int64_t requests, int64_t rows, int64_t table_width, 
  *   rotation   if d_inv_freq, fp32 [head_dim / 2], is not NULL: pair i of each query and key head turns by the angle
  *              position * inv_freq[i] (the product is exact enough at any position): (a, b) to (a cos - b sin, b cos + a sin).
  *              A pair is the elements i, i + head_dim / 2 (DMR_ROPE_HALVES) or 2 i, 2 i + 1 (DMR_ROPE_ADJACENT).
- * Queries go to d_q, bf16 [rows][q_heads head_dim]; keys and values of row t to slot d_slots[t] of the cache; a row whose slot is
+ * Queries go to d_q, bf16 [rows][q_heads head_dim], apart from d_qkv; keys and values of row t to slot d_slots[t] of the cache; a row whose slot is
  * negative or not in the cache is not written there.  Slots of one call are distinct.  d_positions may be NULL without a rotation.
  */
 typedef enum {

@@ -7,6 +7,7 @@ library is missing or a call is refused, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -496,6 +497,13 @@ def _refuse(dev: int, *tensors):
     raise ValueError("a tensor of this call cannot be used")
 
 
+def _for(stream):
+    """Where a call on ``stream`` makes its own tensors: they are filled, and later reused, in that stream's order."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
 class KvCache:
     """One layer's keys and values in pages: the pools of ``dmr_kv_cache_t``, bf16 or float8_e4m3fn (16-byte pieces of ``pc``
     elements), k ``[pages][kv_heads][page_tokens / 16][head_dim / pc][16][pc]``, v ``[pages][kv_heads][page_tokens / 16][16 / pc][head_dim][pc]``."""
@@ -547,7 +555,8 @@ def dmr_kv_assign(new_tokens: torch.Tensor, lens: torch.Tensor, free_pages: torc
     if rows < 0:
         raise ValueError("rows must not be negative")
     if out is None:
-        out = tuple(torch.empty(m, dtype=torch.int32, device=lens.device) for m in (n + 1, n, rows, rows, 2))
+        with _for(stream):
+            out = tuple(torch.empty(m, dtype=torch.int32, device=lens.device) for m in (n + 1, n, rows, rows, 2))
     start, kv_lens, positions, slots, left = out
     if start.numel() != n + 1 or kv_lens.numel() != n or positions.numel() != rows or slots.numel() != rows or left.numel() != 2:
         raise ValueError("out must be query_start [requests + 1], kv_lens [requests], positions [rows], slots [rows], left [2]")
@@ -589,7 +598,8 @@ def dmr_kv_append(cache: KvCache, qkv: torch.Tensor, q_heads: int, positions: to
     if cache.device != dev:
         raise ValueError("the cache must be on the current device")
     if out is None:
-        out = torch.empty((rows, q_heads * D), dtype=torch.bfloat16, device=qkv.device)
+        with _for(stream):
+            out = torch.empty((rows, q_heads * D), dtype=torch.bfloat16, device=qkv.device)
     elif out.shape != (rows, q_heads * D):
         raise ValueError("out must be [rows][q_heads head_dim]")
     f32, i32 = torch.float32, torch.int32
@@ -634,7 +644,8 @@ def dmr_attn_paged(cache: KvCache, q: torch.Tensor, q_heads: int, query_start: t
     if cache.device != dev:
         raise ValueError("the cache must be on the current device")
     if out is None:
-        out = torch.zeros((rows, width), dtype=torch.bfloat16, device=q.device)
+        with _for(stream):
+            out = torch.zeros((rows, width), dtype=torch.bfloat16, device=q.device)
     elif out.shape != (rows, width):
         raise ValueError("out must be [rows][q_heads head_dim]")
     i32 = torch.int32
@@ -649,7 +660,8 @@ def dmr_attn_paged(cache: KvCache, q: torch.Tensor, q_heads: int, query_start: t
     if workspace is None:
         need = dmr_attn_paged_workspace_bytes(rows, n, q_heads, cache.kv_heads, D, max_query)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)    # device memory only
+            with _for(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)    # device memory only
     status = lib().dmr_attn_paged(cache._ref, q.data_ptr(), rows, q_heads, n, query_start.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr(),
                                   columns, max_query, scale, out.data_ptr(), None if workspace is None else workspace.data_ptr(),
                                   0 if workspace is None else workspace.numel(),

@@ -114,8 +114,9 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
         // batch gets finer parts, so that the last ones to start end soon: 96 x 1..8100 287 us with 96 to a head, 268 with 256.
         const int64_t wanted = (e4m3 ? 512 : 1024) / kv_heads;
         // no split, and no second launch, where the table is short (one request of 256 keys 4.8 us against 7.3; of 1003 13.1 against
-        // 8.1, as one CU reads 40 bytes a ns at most) or the requests fill the chip many times over
-        p.split = requests * kv_heads < 8192 && capacity > 256;
+        // 8.1, as one CU reads 40 bytes a ns at most) or the requests fill the chip several times over, where a workgroup's sums over
+        // all their lengths would cost more than an even end gains
+        p.split = capacity > 256 && requests <= 512 && requests * kv_heads < 2048;
         p.parts = p.split ? (int)std::max<int64_t>(1, std::max(wanted, 2 * requests)) : 0;
         p.items = requests + p.parts;
         return p;

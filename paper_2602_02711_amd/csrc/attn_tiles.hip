@@ -64,8 +64,9 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     const int seen = rq.keys - rq.n + token + 1;              // keys this lane's query sees
     auto seen_by = [&](int r) { return rq.keys - rq.n + min(r, rows - 1) / a.G + 1; };
     const int most = seen_by(row0 + kRows - 1);               // the tile's last row
-    const int wave_least = seen_by(row0 + 32 * wave);
-    const int wave_most = row0 + 32 * wave < rows ? seen_by(row0 + 32 * wave + 31) : 0;
+    // and the first and the last of the wave's; a wave without rows stages what the others read
+    const bool any = row0 + 32 * wave < rows;
+    const int wave_least = any ? seen_by(row0 + 32 * wave) : 0, wave_most = any ? seen_by(row0 + 32 * wave + 31) : 0;
     const int units = most > 0 ? (most + kUnit - 1) / kUnit : 0;
     const int u0 = (int)((int64_t)units * part / a.parts), u1 = (int)((int64_t)units * (part + 1) / a.parts);
 

@@ -196,3 +196,35 @@ def test_two_calls_at_once_on_two_streams():
             assert ((got.double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs() + 2.0 ** -7 * want.double().abs().amax()).all()
             a_end = int(st[3])
             assert (outs[0][a_end:] == 0).all() and (outs[1][:a_end] == 0).all()
+
+
+def test_tensors_that_a_call_makes_belong_to_its_stream():
+    """Outputs and workspaces made by the binding are filled and reused in the order of the stream that the call names, while the current
+    stream is busy and allocates the same sizes."""
+    p = Program(6, 40, "bf16", "w4")
+    p.buffers(6 * 90)
+    p.new.fill_(90)
+    hidden(p, 3, 540)
+    p.run(90)
+    torch.cuda.synchronize()
+    args = (p.cache, p.q[89::90].contiguous(), HEADS, torch.arange(7, dtype=torch.int32, device=DEV), p.lens, p.table, 1, SCALE)
+    want = dmr.dmr_attn_paged(*args)
+    want_q = dmr.dmr_kv_append(p.cache, p.qkv, HEADS, p.step[2], torch.full_like(p.step[3], -1), p.gq, p.gk, EPS, p.freq)
+    slow = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        for _ in range(4):
+            for _ in range(3):
+                slow = (slow @ slow).clamp_(-1, 1)                   # the current stream falls behind
+            got = dmr.dmr_attn_paged(*args, stream=stream)
+            side.synchronize()
+            assert torch.equal(got, want)
+            del got
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    none = torch.full_like(p.step[3], -1)
+    torch.cuda.synchronize()
+    q = dmr.dmr_kv_append(p.cache, p.qkv, HEADS, p.step[2], none, p.gq, p.gk, EPS, p.freq, stream=side)
+    side.synchronize()
+    assert torch.equal(q, want_q)
