@@ -99,9 +99,9 @@ __device__ __forceinline__ void norm_and_turn(const AppendArgs &a, const uint4 &
 __device__ __forceinline__ uint4 as_bf16(const float (&x)[8]) {
     return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
-// Four values to e4m3, to nearest even, past the range to the largest.
+// Four values to e4m3, to nearest even, past the range to the largest; NaN stays NaN (a median of three would make it -448).
 __device__ __forceinline__ uint32_t as_e4m3(float a, float b, float c, float d, float inv) {
-    auto range = [&](float v) { return __builtin_amdgcn_fmed3f(v * inv, -448.f, 448.f); };
+    auto range = [&](float v) { return __builtin_elementwise_maximum(__builtin_elementwise_minimum(v * inv, 448.f), -448.f); };
     const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(range(a), range(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(range(c), range(d), lo, true);
 }

@@ -117,6 +117,33 @@ def test_values_past_the_range_of_8_bits_saturate():
     run((qkv * 40, None, None, pos, slots, pages), 2, 2, 64, 16, "e4m3", "none")
 
 
+@pytest.mark.parametrize("rows", [40, 700])
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_elements_that_are_no_numbers_stay_so(rows, cache):
+    """NaN is NaN in the cache too, and infinities are the largest of 8 bits; the elements beside them are right."""
+    heads, kv_heads, dim, page = 2, 2, 64, 16
+    qkv, _, _, pos, slots, pages = case(14, rows, heads, kv_heads, dim, page, cache, norm=False)
+    slots = torch.arange(5, 5 + rows, dtype=torch.int32)
+    odd = torch.zeros(qkv.shape, dtype=torch.bool)
+    odd[::7, heads * dim::5] = True
+    values = torch.tensor([float("nan"), float("inf"), -float("inf")], dtype=torch.bfloat16)
+    qkv[odd] = values[torch.arange(int(odd.sum())) % 3]
+    scale = 1.0 if cache == "bf16" else 0.25
+    pool = dmr.KvCache.empty(pages + 1, page, kv_heads, dim, ref.dtype_of(cache), scale, scale)
+    dmr.dmr_kv_append(pool, to(qkv), heads, None, to(slots))
+    k, v = ref.unpack(ref.raw(pool.k.cpu()), ref.raw(pool.v.cpu()))
+    at = slots.long()
+    got = torch.cat([t.reshape(-1, kv_heads * dim)[at].contiguous().view(ref.dtype_of(cache)).double() for t in (k, v)], 1)
+    want = qkv[:, heads * dim:].double() / scale
+    if cache == "e4m3":
+        want = want.clamp(-448, 448)
+    assert torch.equal(got.isnan(), want.isnan())
+    tol = torch.zeros_like(want) if cache == "bf16" else 2.0 ** -4 * want.abs() + 2.0 ** -10
+    fine = want.isfinite()
+    assert ((got - want).abs()[fine] <= tol[fine]).all()
+    assert torch.equal(got[want.isinf()], want[want.isinf()])
+
+
 @pytest.mark.parametrize("rows", [3, 600])
 def test_cache_past_32_bits_of_bytes(rows):
     """Pages whose bytes lie past 2^32 in a pool of 4.4 GB."""
