@@ -215,6 +215,23 @@ def test_repeated_and_captured(news, lens, cache):
         assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("news,lens", [([3, 1, 5], [3, 700, 2000]), ([90, 40], [400, 1040])])
+def test_queries_that_are_no_numbers_spoil_only_their_own_rows(news, lens, cache):
+    heads, kv_heads, dim = 4, 2, 64
+    pool, q, keys, table = build(24, news, lens, heads, kv_heads, dim, 32, cache)
+    rows, start = sum(news), np.concatenate([[0], np.cumsum(news)])
+    bad = torch.zeros(rows, heads, dtype=torch.bool)
+    bad[1, 2] = bad[rows - 2, 0] = True
+    odd = q.view(rows, heads, dim).clone()
+    odd[1, 2, 7], odd[rows - 2, 0, 0] = float("nan"), float("inf")
+    out = dmr.dmr_attn_paged(pool, odd.view(rows, -1).to(DEV), heads, dev(start), dev(lens), dev(table), max(news), dim ** -0.5)
+    want, tol = expect(q, keys, news, heads, dim, dim ** -0.5, rounding_of_weights(max(news), heads, kv_heads))
+    got = out.cpu().double().view(rows, heads, dim)
+    assert ((got - want).abs() <= tol)[~bad].all()
+    assert got[1, 2].isnan().all()
+
+
 def test_pages_shared_by_requests():
     """Two requests whose first pages are the same ones."""
     pool, q, keys, table = build(21, [1, 1], [200, 130], 4, 2, 64, 64, "bf16")
