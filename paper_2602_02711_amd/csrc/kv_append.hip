@@ -136,7 +136,7 @@ __device__ __forceinline__ void store_value(const AppendArgs &a, const Place &at
         reinterpret_cast<uint16_t *>(a.v)[at.block * (16 * D) + (at.tok >> 3) * (D * 8) + d * 8 + (at.tok & 7)] = v;
 }
 
-constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.2 / 8.6 us (e4m3 7.8 / 10.4), 768 12.9 / 9.3 (11.9 / 10.8)
+constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.2 / 8.6 us (e4m3 7.8 / 10.4), 768 12.9 / 9.3 (11.9 / 11.3)
 
 // Few rows: a workgroup has 256 / (D / 8) heads of one row.
 template <int D, bool E4M3, bool ADJACENT>
