@@ -257,7 +257,7 @@ dmr_status_t dmr_kv_assign(int64_t requests, int64_t rows, int64_t table_width, 
  * The output of the fused qkv projection to queries, and to keys and values in the cache.  d_qkv is bf16
  * [rows][(q_heads + 2 kv_heads) head_dim]: the query heads, the key heads, the value heads.  In fp32, rounded once at the end:
  *   norm       y = x * gamma / sqrt(mean(x^2) + eps) over each query (key) head, if d_gamma_q (d_gamma_k), bf16 [head_dim], is
- *              not NULL; a head of zeros stays zeros
+ *              not NULL, at any size of its elements; a head of zeros stays zeros (also with eps 0), one with a NaN is NaN throughout
  *   rotation   if d_inv_freq, fp32 [head_dim / 2], is not NULL: pair i of each query and key head turns by the angle
  *              position * inv_freq[i] (the product is exact enough at any position): (a, b) to (a cos - b sin, b cos + a sin).
  *              A pair is the elements i, i + head_dim / 2 (DMR_ROPE_HALVES) or 2 i, 2 i + 1 (DMR_ROPE_ADJACENT).

@@ -57,7 +57,27 @@ struct Turn {
     }
 };
 
-// A lane's 8 elements of query or key head h, normed and turned.
+// mean(x^2) + eps of the head whose elements the group's lanes hold, eight each; x may come back times a power of two, and the result then
+// is of those.  A square below 2^-100 has lost bits of its terms and one above 2^100 may have overflowed: there the elements are brought
+// to where neither happens (the smallest, 2^-133, to 2^-33; the largest, below 2^128, to 2^58) and summed again.
+template <int LANES>
+__device__ __forceinline__ float head_square(const uint4 &raw, float eps, float (&x)[8]) {
+    constexpr float kPer = 1.0f / (8 * LANES);
+    float square = fmaf(head_sum<LANES>(sumsq_piece(raw)), kPer, eps);
+    if (!(square >= 0x1p-100f && square <= 0x1p100f)) {      // or no number; lanes of a head come here together
+        const float by = square > 1.f ? 0x1p-70f : 0x1p100f;
+        float own = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] *= by;
+            own = fmaf(x[e], x[e], own);
+        }
+        square = fmaf(head_sum<LANES>(own), kPer, eps * by * by);
+    }
+    return square;
+}
+
+// A lane's 8 elements of query or key head h, normed and turned.  A head of zeros stays zeros, one with a NaN is NaN throughout.
 template <int D, bool ADJACENT>
 __device__ __forceinline__ void norm_and_turn(const AppendArgs &a, const uint4 &raw, int h, int lane, const Turn<D, ADJACENT> &turn, float (&x)[8]) {
     constexpr int LANES = D / 8;
@@ -69,7 +89,7 @@ __device__ __forceinline__ void norm_and_turn(const AppendArgs &a, const uint4 &
     }
     const uint16_t *gamma = h < a.q_heads ? a.gamma_q : a.gamma_k;
     if (gamma) {
-        const float scale = rms_scale(head_sum<LANES>(sumsq_piece(raw)), 1.0f / D, a.eps);
+        const float square = head_square<LANES>(raw, a.eps, x), scale = square == 0.f ? 0.f : __builtin_amdgcn_rsqf(square);
         const uint4 g = reinterpret_cast<const uint4 *>(gamma)[lane];
         const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll

@@ -157,3 +157,48 @@ def test_cache_past_32_bits_of_bytes(rows):
     _, (wk, sk), wv = ref.append(qkv, 8, heads, dim, gq, gk, 1e-6, inv_freq(dim), False, pos)
     close(k.reshape(-1, heads, dim)[-rows:].contiguous().view(torch.bfloat16), wk, ref.BF16_STEP * wk.abs() + NEAR * sk, "k")
     assert torch.equal(v.reshape(-1, heads, dim)[-rows:].contiguous().view(torch.bfloat16).double(), wv)
+
+
+@pytest.mark.parametrize("rows", [40, 700])
+@pytest.mark.parametrize("rope", ["halves", "adjacent", "none"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_normed_head_with_a_nan_is_nan_and_no_other(dim, rope, rows):
+    """Its mean of squares is NaN, so all of its elements are; the same rows without it say what the other heads are."""
+    heads, kv_heads, page = 4, 2, 16
+    qkv, gq, gk, pos, _, pages = case(15, rows, heads, kv_heads, dim, page, "bf16")
+    slots = torch.arange(rows, dtype=torch.int32)
+    freq = None if rope == "none" else to(inv_freq(dim))
+
+    def call(x):
+        pool = dmr.KvCache.empty(pages, page, kv_heads, dim)
+        q = dmr.dmr_kv_append(pool, to(x), heads, to(pos), to(slots), to(gq), to(gk), 1e-6, freq, rope == "adjacent")
+        k, v = ref.unpack(ref.raw(pool.k.cpu()), ref.raw(pool.v.cpu()))
+        k, v = (t.reshape(-1, kv_heads, dim)[:rows].contiguous().view(torch.bfloat16) for t in (k, v))
+        return q.cpu().view(rows, heads, dim), k, v
+
+    odd = qkv.clone().view(rows, heads + 2 * kv_heads, dim)
+    hit = torch.zeros(rows, heads + kv_heads, dtype=torch.bool)
+    hit[::3, 1] = hit[::5, heads] = hit[rows - 1, 0] = True
+    for t, h in hit.nonzero().tolist():
+        odd[t, h, (7 * t + h) % dim] = float("nan")
+    plain, got = call(qkv), call(odd.view(rows, -1))
+    hits = (hit[:, :heads], hit[:, heads:], torch.zeros(rows, kv_heads, dtype=torch.bool))
+    for p, g, at in zip(plain, got, hits):
+        assert g[at].isnan().all() and torch.equal(g[~at], p[~at])
+
+
+@pytest.mark.parametrize("rows", [24, 700])
+@pytest.mark.parametrize("power,eps", [(p, e) for p in (-133, -100, -66, -62, -51, 49, 62, 64, 120) for e in (0.0, 2.0 ** -132, 1e-6)
+                                       if p > -133 or e < 1e-6])
+def test_norms_of_very_small_and_very_large_heads(power, eps, rows):
+    """Elements whose squares are past the ends of fp32, down to the smallest of bf16.  (2^-133 beside an eps of 1e-6 gives results with fewer
+    than eight bits, which the tolerances do not count.)"""
+    heads, kv_heads, dim, page = 4, 2, 128, 32
+    gen = torch.Generator().manual_seed(16)
+    qkv, gq, gk, pos, slots, pages = case(17, rows, heads, kv_heads, dim, page, "bf16")
+    x = qkv.double() * 2.0 ** power
+    x = x.view(rows, -1, dim)
+    x[1::4] = 0                                                           # heads of zeros, heads of one element, and ordinary ones beside them
+    x[2::4, :, 1:] = 0
+    x[3::4, 1] = torch.randn(x[3::4, 1].shape, generator=gen, dtype=torch.float64)
+    run((x.view(rows, -1).bfloat16(), gq, gk, pos, slots, pages), heads, kv_heads, dim, page, "bf16", "halves", eps=eps)
