@@ -211,8 +211,8 @@ dmr_status_t dmr_qlinear_bf16_forward_fused(const uint16_t *d_w, dmr_prologue_t 
  *
  * The int32 arrays of these calls need 4-byte alignment only, so that a call can take part of a batch from any request on.
  * page_tokens: 16, 32, 64, 128 or 256.  head_dim: 64 or 128.  pages * page_tokens below 2^31.  DMR_KV_BF16 keeps the elements as
- * they are (both scales 1); DMR_KV_E4M3 keeps x / scale in 8 bits (e4m3, to nearest even, past 448 the largest, NaN as NaN), one
- * positive scale for the keys and one for the values of the layer.
+ * they are (both scales 1); DMR_KV_E4M3 keeps x / scale, the quotient in fp32, in 8 bits (e4m3, to nearest even, past 448 the
+ * largest, NaN as NaN), one positive scale for the keys and one for the values of the layer.
  */
 typedef enum {
     DMR_KV_BF16 = 0,

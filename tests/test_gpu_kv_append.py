@@ -202,3 +202,25 @@ def test_norms_of_very_small_and_very_large_heads(power, eps, rows):
     x[2::4, :, 1:] = 0
     x[3::4, 1] = torch.randn(x[3::4, 1].shape, generator=gen, dtype=torch.float64)
     run((x.view(rows, -1).bfloat16(), gq, gk, pos, slots, pages), heads, kv_heads, dim, page, "bf16", "halves", eps=eps)
+
+
+@pytest.mark.parametrize("rows", [40, 1024])
+@pytest.mark.parametrize("scale", [0.05, 0.25, 7 / 256, 13 / 256, 15 / 256, 61 / 256, 7.0])
+def test_eight_bits_of_a_value_over_its_scale(scale, rows):
+    """Every finite bf16 value, or (fewer rows) those whose quotients are in range, over scales of few bits, which give ties, and others: the quotient
+    in fp32, to nearest even."""
+    heads, kv_heads, dim, page = 1, 1, 64, 32
+    step = torch.tensor(scale, dtype=torch.float32)
+    every = torch.arange(2 ** 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    every[~every.isfinite()] = 0
+    if rows < 1024:
+        near = (every.abs() < 448 * scale * 1.1) & (every.abs() > scale / 2048) & (every > 0)
+        every = every[near][-rows * dim:]
+        every = torch.cat([every, -every, torch.zeros(rows * dim, dtype=torch.bfloat16)])[:rows * dim]
+    x = every.view(rows, 1, dim).expand(rows, 3, dim).reshape(rows, -1).contiguous()
+    pool = dmr.KvCache.empty(rows // page + 1, page, kv_heads, dim, torch.float8_e4m3fn, scale, scale)
+    dmr.dmr_kv_append(pool, to(x), heads, None, torch.arange(rows, dtype=torch.int32, device=DEV))
+    want = (every.float() / step).clamp(-448, 448).to(torch.float8_e4m3fn).view(rows, dim)
+    for got in ref.unpack(ref.raw(pool.k.cpu()), ref.raw(pool.v.cpu())):
+        got = got.reshape(-1, dim)[:rows].contiguous().view(torch.float8_e4m3fn)
+        assert torch.equal(got.double(), want.double())
