@@ -43,6 +43,10 @@ __device__ __forceinline__ Request request_at(const AttnArgs &a, int b) {
     return r;
 }
 
+// Units of UNIT keys in `keys` of them, which may be up to 2^31 - 16: the sum before the division passes 31 bits.
+template <int UNIT>
+__device__ __forceinline__ int units_in(int keys) { return (int)(((uint32_t)keys + (UNIT - 1)) / UNIT); }
+
 // First byte of a block of 16 tokens of one head: `block` of the request whose row of the table is given.
 template <int BLOCK_BYTES>
 __device__ __forceinline__ int64_t block_offset(const AttnArgs &a, const int32_t *row, int block, int head) {
@@ -115,7 +119,8 @@ template <int UNIT>
 __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int lane) {
     uint64_t total = 0;
     uint32_t longest = 0, some = 0;
-    auto units_of = [](const Request &r) { return (uint32_t)(r.n > 0 ? (r.keys + UNIT - 1) / UNIT : 0); };
+    // (64 requests of 2^31 keys each would have 2^32 units: one less for such a request keeps a round's sum in 32 bits)
+    auto units_of = [](const Request &r) { return r.n > 0 ? std::min((uint32_t)units_in<UNIT>(r.keys), (1u << 26) - 1) : 0u; };
     auto request_of = [&](int i) { return i < a.requests ? request_at(a, i) : Request{0, 0, 0}; };
     Request r;      // of this lane, in the round at hand: up to 64 requests are read once
     for (int base = 0; base < a.requests; base += 64) {

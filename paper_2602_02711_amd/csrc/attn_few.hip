@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256, E4M3 && D == 128 && NQ == 2 ? 1 : 2) void attn
     const int rows = min(rq.n * a.G, ROWS);
     if (sh.b < 0 || rows == 0) return;
     const int32_t *pages = a.table + (int64_t)sh.b * a.width;
-    const int units = (rq.keys + UNIT - 1) / UNIT;
+    const int units = units_in<UNIT>(rq.keys);
     const int u0 = (int)((int64_t)units * sh.part / sh.parts), u1 = (int)((int64_t)units * (sh.part + 1) / sh.parts);
     const int last_block = max(rq.keys - 1, 0) >> 4;
     const int first_seen = rq.keys - rq.n + 1;       // keys that the first row sees; later ones see more
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256, E4M3 && D == 128 && NQ == 2 ? 1 : 2) void attn
         }
         if constexpr (MORE) load_keys();
         const int first = u * UNIT;
-        const bool masked = first + UNIT > first_seen;
+        const bool masked = first > first_seen - UNIT;
         Frag ph[NQ][STEPS], pl[NQ][STEPS];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, E4M3 && D == 128 && NQ == 2 ? 1 : 2) void attn
         }
         // values of slots behind the last key may hold anything, and 0 x NaN is NaN
         uint32_t keep[STEPS][4];
-        const bool ragged = first + UNIT > rq.keys;
+        const bool ragged = first > rq.keys - UNIT;
         if (ragged) {
 #pragma unroll
             for (int st = 0; st < STEPS; ++st)

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256, 2) void attn_tiles_kernel(AttnArgs a) {
     // and the first and the last of the wave's; a wave without rows stages what the others read
     const bool any = row0 + 32 * wave < rows;
     const int wave_least = any ? seen_by(row0 + 32 * wave) : 0, wave_most = any ? seen_by(row0 + 32 * wave + 31) : 0;
-    const int units = most > 0 ? (most + kUnit - 1) / kUnit : 0;
+    const int units = most > 0 ? units_in<kUnit>(most) : 0;
     const int u0 = (int)((int64_t)units * part / a.parts), u1 = (int)((int64_t)units * (part + 1) / a.parts);
 
     Frag q[KS];

@@ -267,3 +267,27 @@ def test_cache_past_32_bits_of_bytes():
         out = dmr.dmr_attn_paged(pool, q, heads, dev([0, n]), dev([700]), dev([[pages - 3, pages - 2, pages - 1]]), n, 0.1)
         want, tol = expect(q.cpu(), [(kb, vb)], [n], heads, dim, 0.1, r)
         assert ((out.cpu().double().view(n, heads, dim) - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 5, 40])
+def test_as_many_keys_as_a_table_can_name(new, cache):
+    """A request of 2^31 - 16 keys.  All but the last 128 are those of one page, whose weights are below 2^-250 of the others'."""
+    page, dim, heads, width, last = 16, 64, 1, (2 ** 31 - 1) // 16, 8
+    gen = torch.Generator().manual_seed(31)
+    ks, vs = (1.0, 1.0) if cache == "bf16" else (0.25, 0.25)
+    dt = ref.dtype_of(cache)
+    k, v = (torch.randn((last + 1) * page, 1, dim, generator=gen).div(s).clamp(-448, 448).to(dt) for s in (ks, vs))
+    far = torch.zeros(page, 1, dim)
+    far[:, :, 0] = -100 / ks
+    k = torch.cat([far, k[page:].float()])
+    kp, vp = ref.pack(k.view(last + 1, page, 1, dim), v.float().view(last + 1, page, 1, dim), cache)
+    pool = dmr.KvCache(kp.to(dt).to(DEV), vp.to(dt).to(DEV), ks, vs)
+    q = torch.randn(new, dim, generator=gen).bfloat16()
+    q[:, 0] = 16
+    table = torch.zeros((1, width), dtype=torch.int32, device=DEV)
+    table[0, -last:] = torch.arange(1, last + 1, dtype=torch.int32, device=DEV)
+    out = dmr.dmr_attn_paged(pool, q.to(DEV), heads, dev([0, new]), dev([width * page]), table, new, dim ** -0.5)
+    keys = [(k[page:].double() * ks, v[page:].double() * vs)]
+    want, tol = expect(q, keys, [new], heads, dim, dim ** -0.5, rounding_of_weights(new, heads, 1))
+    assert ((out.cpu().double().view(new, heads, dim) - want).abs() <= tol).all()
