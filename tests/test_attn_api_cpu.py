@@ -121,3 +121,35 @@ def test_binding_checks_before_the_library():
         b.KvCache.empty(4, 16, 2, 128, torch.float16, device="cpu")
     with pytest.raises(ValueError):
         b.KvCache.empty(4, 24, 2, 128, device="cpu")
+
+
+def aligned(n):
+    return -(-n // 256) * 256
+
+
+# rows to a key head, and requests x key heads up to where a batch is not split any more; then batches of tiles up to one for each CU
+FEW = [(255, 32, 8, 128, 1), (255, 64, 8, 128, 4), (512, 12, 3, 128, 8), (512, 3, 3, 64, 17), (1, 32, 1, 128, 1), (511, 32, 4, 64, 2), (200, 7, 1, 128, 3)]
+TILES = [(31, 32, 8, 128, 30), (1, 32, 8, 128, 1024), (1, 1, 1, 64, 33), (63, 16, 4, 64, 30), (40, 8, 1, 128, 50), (7, 64, 2, 128, 20)]
+
+
+@pytest.mark.parametrize("requests,heads,kv_heads,dim,most", FEW + TILES)
+def test_workspaces_are_as_large_as_the_largest_plan(lib, requests, heads, kv_heads, dim, most):
+    """The query answers for any table and either cache type: what the parts of the batch can need at most, no less than any call asks for, and
+    not much more."""
+    rows = requests * most
+    need = lib.dmr_attn_paged_workspace_bytes(rows, requests, heads, kv_heads, dim, most)
+    to_a_head = most * (heads // kv_heads)
+    if to_a_head <= 32:
+        tile, items = (16 if to_a_head <= 16 else 32), requests + max(1024 // kv_heads, 2 * requests)
+    else:
+        tile, tiles = 128, min(requests * -(-to_a_head // 128), rows * (heads // kv_heads) // 128 + requests)
+        items = tiles * min(32, max(1, 512 // (tiles * kv_heads)))
+        assert items > tiles                               # these cases are split
+    parts = items * kv_heads * tile
+    assert need == aligned(parts * dim * 4) + aligned(parts * 8) + (requests * 8 if tile < 128 else 0)
+    # a call that passes every check finds no GPU here
+    for kind in (b.DMR_KV_BF16, b.DMR_KV_E4M3):
+        for width in (1, 2, 4, 5, 8, 16, 33, 64, 100, 300, 1000, 5000, 2 ** 20, 2 ** 24):
+            c = cache(kv_heads=kv_heads, head_dim=dim, type=kind)
+            got = attend(lib, c, rows=rows, heads=heads, requests=requests, width=width, most=most, ws_bytes=need)
+            assert got == b.DMR_ERR_HIP, (width, got)
