@@ -279,16 +279,24 @@ dmr_status_t dmr_kv_append(const dmr_kv_cache_t *cache, const uint16_t *d_qkv, i
  * 0 .. d_kv_lens[b] - n + i, and query head h the keys of head h / (q_heads / kv_heads):
  *   out[i][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * (q[i][h] . k_j))
  * scale is positive.  d_q and d_out are bf16 [rows][q_heads head_dim] and apart, d_block_table is [requests][table_width].  A row that sees no key is 0; rows before
- * the first request and behind the last are left as they were.  max_query is at least the largest n (rows of a request past it
- * are not computed); it chooses the kernel, so a decode step passes 1.  Scores, sums and outputs are held in fp32; of the weights
+ * the first request and behind the last are left as they were.  max_query is at least the largest n (what the rows of a request past it
+ * get, if anything, is not defined); it chooses the kernel, so a decode step passes 1.  Scores, sums and outputs are held in fp32; of the weights
  * p_j the product with the values takes 16 bits where a key head has up to 32 rows of a request (max_query q_heads / kv_heads),
  * and 8, as many as the values have, where it has more; there the sum that divides it takes the same 8.
  * Lengths past the table are read as its width, entries of the table outside the cache as its first or last page; slots
  * behind a request's last key may hold anything, NaN included.  Non-finite keys and values that a request does hold are outside
  * the contract.
  * d_ws as dmr_attn_paged_workspace_bytes says: partial results where the keys of a request are split over workgroups.  It may
- * arrive uninitialised.  The lengths are read on the device alone: a captured call serves any lengths that `rows`, the table
- * and max_query admit.
+ * arrive uninitialised.  A program that serves batches of several sizes from one workspace asks for each: a smaller batch is split finer
+ * and may need more.  At most 2^20 requests and 2^22 rows; tiles x kv_heads below 2^24 (a tile is a request with up to 32 rows to a key
+ * head, else 128 of them); rows x q_heads / kv_heads and table_width x page_tokens below 2^31.
+ * The lengths are read on the device alone: a captured call serves any lengths that `rows`, the table and max_query admit.  What the
+ * host knows chooses how a call is split, and a batch can be better served by two calls, each on its part of the arrays:
+ *   - up to 32 rows to a key head, keys are split by the lengths on the device; past 512 requests, and from requests x kv_heads = 2048
+ *     on, not at all: there a history many times the others' goes in a call of its own;
+ *   - above that, every tile of 128 rows has the same number of parts, by the number of tiles and the tokens that the table can name,
+ *     not by lengths: single tokens on long histories beside a chunk go in a call of their own with max_query 1, and a table
+ *     no wider than the longest request needs saves short prompts parts that they have no use for.
  */
 size_t dmr_attn_paged_workspace_bytes(int64_t rows, int64_t requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                                       int64_t max_query);

@@ -633,7 +633,8 @@ def dmr_attn_paged(cache: KvCache, q: torch.Tensor, q_heads: int, query_start: t
                    block_table: torch.Tensor, max_query: int, scale: float, out: torch.Tensor | None = None,
                    workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Causal attention of rows q [rows][q_heads head_dim] over their requests' keys in the cache.  A new ``out`` is zeroed, since
-    rows of no request are not written."""
+    rows of no request are not written; a given one is apart from ``q``.  Single tokens on long histories beside a chunk are better
+    served by a call of their own with ``max_query`` 1."""
     dev = torch._C._cuda_getDevice()
     n, D = kv_lens.numel(), cache.head_dim
     (rows, width), (requests, columns) = q.shape, block_table.shape

@@ -55,7 +55,8 @@ __device__ __forceinline__ int64_t block_offset(const AttnArgs &a, const int32_t
     return (((((int64_t)page * a.kv_heads + head) << per_page) + (block & ((1 << per_page) - 1)))) * BLOCK_BYTES;
 }
 
-// The same through the scalar cache, for a block that all lanes ask for.
+// The same for a block that all lanes ask for: a scalar load where the compiler can tell that they do (attn_tiles), a vector load where it
+// cannot (attn_few, whose wave index it takes for a lane's own).
 template <int BLOCK_BYTES>
 __device__ __forceinline__ int64_t uniform_block_offset(const AttnArgs &a, const int32_t *row, int block, int head) {
     typedef const __attribute__((address_space(4))) int32_t *constant_i32;
@@ -113,7 +114,7 @@ __device__ __forceinline__ Share share_of_tile(const AttnArgs &a, int tile, int 
 // C = max(kMinUnits, ceil(U / a.parts)), a request of u units has ceil(u / C) parts, one at least: no more than a.parts + requests
 // items, whatever the lengths.  A batch that gives every CU a workgroup and whose longest request is no longer than 3 / 2 of the mean
 // is not split.  Each workgroup forms the same sums from the lengths on the device, so that a captured call splits the lengths
-// of its replay and a ragged batch's longest request decides nothing.
+// of its replay.  (Whether a call is split at all, plan_attn decides from the batch's size.)
 constexpr int kMinUnits = 4;      // a unit for each wave of a workgroup
 template <int UNIT>
 __device__ __forceinline__ Share share_of_item(const AttnArgs &a, int item, int lane) {

@@ -2,8 +2,9 @@
 //
 // A workgroup has all rows of a request to one key head, 16 or 32, and a part of its keys (share_of_item), dealt to its four waves in
 // units of 32, or of 64 e4m3 ones.  Operands go from the cache straight into registers, 16 bytes a lane and whole lines a wave; the keys of the next unit
-// are requested once the scores have used this one's, the values once the outputs have, so a wave always has 4 .. 16 KB in
-// flight and no barrier holds it.  The rows are the columns of 16 x 16 x 32 MFMAs (S^T = K Q^T, O^T += V^T P^T): maximum
+// are requested once the scores have used this one's, the values once the outputs have, 4 .. 16 KB each, and no barrier holds a wave.  Between
+// the scores and the next keys lie the next unit's entries of the block table: vector loads, which return in order, so there, once a
+// unit, a wave waits for its values and then for the table with nothing else in flight, and the other waves of the CU have the memory.  The rows are the columns of 16 x 16 x 32 MFMAs (S^T = K Q^T, O^T += V^T P^T): maximum
 // and sum are per-lane numbers, and a lane's scores are the keys that its value pieces hold.  As the matrix cores have time to
 // spare, the weights enter as two bf16 each, 16 bits.  The waves' results are joined in LDS, the workgroups' by a second kernel.
 #include "attn.hpp"

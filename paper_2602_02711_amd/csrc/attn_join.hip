@@ -108,14 +108,19 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     p.max_tiles = 1;
     if (p.few) {
         p.tile_rows = most <= 16 ? 16 : 32;
-        // Parts: about what the chip holds at once of these workgroups, two (e4m3) to four (bf16, whose waves hold less) a CU.  Between
+        // Parts: about what the chip holds at once of these workgroups, two (e4m3; one with D = 128 and 32 rows, whose parts come in two
+        // rounds) to four (bf16, whose waves hold less) a CU.  Between
         // half and twice that a decode step of the 7B-class decoder varies by 10 %.  us with 512 / 1024 in all: 1 x 32768 keys 27.8 /
         // 29.4 (e4m3 19.1 / 22.7), 16 x 300..9000 62.2 / 58.6 (38.9 / 36.7), 32 x 1003 27.5 / 28.3 (18.6 / 21.6).  A large ragged
         // batch gets finer parts, so that the last ones to start end soon: 96 x 1..8100 287 us with 96 to a head, 268 with 256.
         const int64_t wanted = (e4m3 ? 512 : 1024) / kv_heads;
         // no split, and no second launch, where the table is short (one request of 256 keys 4.8 us against 7.3; of 1003 13.1 against
         // 8.1, as one CU reads 40 bytes a ns at most) or the requests fill the chip several times over, where a workgroup's sums over
-        // all their lengths would cost more than an even end gains
+        // all their lengths, and the join, cost more than an even end gains: us unsplit / split, 256 requests of 8 key heads with 300 keys
+        // each 62 / 79 (e4m3 40 / 70), 1000 193 / 203 (106 / 129), 1 .. 2000 222 / 211 (107 / 149); 512 with 1000 355 / 390 (202 / 289);
+        // 2048 of one head with 1000 169 / 293 (100 / 274).  The price is a batch with a history many times the others', which one
+        // workgroup to a head then reads alone: 256 with 500 keys and one of 32768 499 / 148 (291 / 115), 1 .. 1000 and two
+        // of 131071 1744 / 290 (1067 / 188); 600 of one head, the same two, 1616 / 78 (1013 / 64).
         p.split = capacity > 256 && requests <= 512 && requests * kv_heads < 2048;
         p.parts = p.split ? (int)std::max<int64_t>(1, std::max(wanted, 2 * requests)) : 0;
         p.items = requests + p.parts;
@@ -128,7 +133,9 @@ AttnPlan plan_attn(int64_t rows, int64_t requests, int q_heads, int kv_heads, in
     // Parts: the least estimated time, in ns, among those that two workgroups a CU can serve at once.  A workgroup alone on its CU takes
     // 17 ns for a key of its tile, two take 29 (D = 64: 0.6 of that); joining costs a launch and the partial results' way to memory and
     // back.  us with 1 part / as many as 256 / 512 workgroups: 64 rows over 2000 keys 39 / 19 / 26, 300 over 8000 137 / 63 / 61, 512
-    // over 32768 543 / 311 / 272, 1024 over 1024 25 / 25 / 35, over 16000 288 / 293 / 258, 8 x 12 over 4000 72 / 31 / 43.
+    // over 32768 543 / 311 / 272, 1024 over 1024 25 / 25 / 35, over 16000 288 / 293 / 258, 8 x 12 over 4000 72 / 31 / 43.  The capacity
+    // stands for the longest request: with a table of 131072 tokens instead of one as long as that, 64 over 2000 26 instead of 16, 1024
+    // over 1024 36 instead of 25, 300 over 8000 59 instead of 67, 8192 over 8192 level.
     const int64_t wgs = std::max<int64_t>(1, tiles * kv_heads), most_parts = std::max<int64_t>(1, std::min<int64_t>(32, 2 * kCus / wgs));
     auto estimate = [&](int64_t parts) {
         const double key = (D == 64 ? 0.6 : 1.0) * (wgs * parts <= kCus ? 17.0 : 29.0);

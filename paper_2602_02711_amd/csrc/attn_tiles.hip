@@ -12,7 +12,7 @@
 // slower).  One barrier for each 64 keys; a second workgroup on the CU works through it.
 //
 // Bound by power: 2048 rows over 32768 keys run at 1.7 GHz with the matrix pipes busy 64 % of the cycles, as long bf16 products do;
-// 920 .. 955 us, 1.12 .. 1.16 PFLOP/s, where one of 8192^3 reaches 1.21.  What brought it there, from 1840 us: loads ahead and masks at
+// 910 .. 960 us, 1.11 .. 1.17 PFLOP/s, where one of 8192^3 reaches 1.14 .. 1.28.  What brought it there, from 1840 us: loads ahead and masks at
 // the edges alone, 1072; a loop of its own for units without an edge (the branch inside kept copies of all accumulators) and the
 // maximum looked for only when a sum says so, 9 % less; every operand read from LDS eight MFMAs before its own, 6 %; the tiles with
 // the most keys first, 8 .. 12 % of a causal prompt; priority for the wave that is at its products, 2 %.  Eight waves on the same

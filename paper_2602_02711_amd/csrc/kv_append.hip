@@ -166,7 +166,10 @@ __device__ __forceinline__ void store_value(const AppendArgs &a, const Place &at
         reinterpret_cast<uint16_t *>(a.v)[at.block * (16 * D) + (at.tok >> 3) * (D * 8) + d * 8 + (at.tok & 7)] = v;
 }
 
-constexpr int kTilesFrom = 640;      // rows: 512 of the 7B-class decoder 8.2 / 8.6 us (e4m3 7.8 / 10.4), 768 12.9 / 9.3 (11.9 / 11.3)
+// Rows, as the 7B-class decoder has it (32 + 8 heads of 128; us by rows / by tiles): 512 8.1 / 8.5 (e4m3 7.7 / 10.6), 640 9.3 / 8.7 (9.2 / 10.7), 768
+// 12.8 / 9.3 (11.5 / 11.2).  Wider layouts cross earlier (64 + 8 of 128: 430 rows, e4m3 600), narrower ones later: 768 rows of 28 + 4 of 128 7.4 / 8.5
+// (7.6 / 10.6), of 8 + 2 4.8 / 7.5 (4.3 / 9.6), of 16 + 8 of 64 6.3 / 5.6 (5.2 / 7.3), of 4 + 1 of 64 3.1 / 5.1 (3.4 / 6.9).
+constexpr int kTilesFrom = 640;
 
 // Few rows: a workgroup has 256 / (D / 8) heads of one row.
 template <int D, bool E4M3, bool ADJACENT>
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(256) void append_rows_kernel(AppendArgs a) {
 // together; or 64 rows of one value head, which it turns in LDS: tokens that fill a piece of the cache leave as one store
 // of 16 bytes, the others, at the ends of a run of slots, element by element.  (With a thread's 8 elements of one token stored
 // one by one a wave's store fell into 64 lines: 8192 rows 77 us.)  The projection is read, and queries are written, past the caches:
-// 53 -> 42 us for 8192 rows of the 7B-class decoder, 4.8 TB/s, where a copy of as many bytes takes 39.
+// 53 -> 41 us for 8192 rows of the 7B-class decoder, 4.9 .. 5.0 TB/s, where a copy of as many bytes takes 39 (into e4m3 42 us, 4.4 TB/s).
 constexpr int kHeadsAtOnce = 4, kValueRows = 64;
 template <int D, bool E4M3, bool ADJACENT>
 __global__ __launch_bounds__(256) void append_tiles_kernel(AppendArgs a, int rows, int chunks) {
